@@ -128,7 +128,8 @@ int astro_kvcache_reset(astro_kvcache_t *cache, int32_t stream, int32_t start_fr
  * stream.  k, v: device, un-rotated, [B, n_frames*T, H, D].  Frame number n of a
  * stream (0-based since reset) goes to ring slot n if n < C, else
  * S + (n - S) mod Lw, overwriting -- evicting -- frame n - Lw; keys are rotated
- * at absolute frame index start_frame + n and stored, values copied.
+ * at absolute frame index start_frame + n and stored, values copied.  (bf16: rotated in 64 bits,
+ * rounded to 32 and then to bf16.)
  * With ASTRO_FLAG_WINDOW_RELATIVE the un-rotated keys of arriving sink frames are also
  * copied to k_sink_storage, and once frames are evicted the sinks' keys in the ring are
  * rotated again at start_frame + s + (frames evicted so far) in the same call.

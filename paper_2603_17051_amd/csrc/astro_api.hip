@@ -23,6 +23,8 @@ struct astro_kvcache {
   double* d_inv_freq_t = nullptr;
   float2* d_tab_h = nullptr;
   float2* d_tab_w = nullptr;
+  double2* d_tab_h64 = nullptr;
+  double2* d_tab_w64 = nullptr;
   int device = -1;
   int n_cus = 256;
   // What the last rotation pre-pass left in a caller's workspace (ASTRO_FLAG_REUSE_STAGED): the
@@ -60,6 +62,8 @@ DevGeom dev_geom(const astro_kvcache* c, int group = 1) {
   d.inv_freq_t = c->d_inv_freq_t;
   d.tab_h = c->d_tab_h;
   d.tab_w = c->d_tab_w;
+  d.tab_h64 = c->d_tab_h64;
+  d.tab_w64 = c->d_tab_w64;
   return d;
 }
 
@@ -396,28 +400,34 @@ int astro_kvcache_create(const astro_kvcache_desc_t* desc, astro_kvcache_t** out
   if (!c) return ASTRO_ERR_INVALID_ARG;
   c->k_sink_storage = desc->k_sink_storage;
   if (!g.host_only) {
-    // rotary tables in fp64, rounded once to fp32
+    // rotary tables in fp64, and rounded once to fp32
     std::vector<double> inv_t(g.n_t > 0 ? g.n_t : 1, 0.0);
     for (int j = 0; j < g.n_t; ++j) inv_t[j] = std::pow(g.rope_base, -(double)j / g.n_t);
     std::vector<float2> th((size_t)g.gh * (g.n_h > 0 ? g.n_h : 1)), tw((size_t)g.gw * (g.n_w > 0 ? g.n_w : 1));
-    for (int r = 0; r < g.gh; ++r)
-      for (int j = 0; j < g.n_h; ++j) {
-        const double a = (double)r * std::pow(g.rope_base, -(double)j / g.n_h);
-        th[(size_t)r * g.n_h + j] = make_float2((float)std::cos(a), (float)std::sin(a));
-      }
-    for (int w = 0; w < g.gw; ++w)
-      for (int j = 0; j < g.n_w; ++j) {
-        const double a = (double)w * std::pow(g.rope_base, -(double)j / g.n_w);
-        tw[(size_t)w * g.n_w + j] = make_float2((float)std::cos(a), (float)std::sin(a));
-      }
+    std::vector<double2> th64(th.size()), tw64(tw.size());
+    auto fill = [&](int positions, int pairs, std::vector<double2>& wide, std::vector<float2>& tab) {
+      for (int at = 0; at < positions; ++at)
+        for (int j = 0; j < pairs; ++j) {
+          const double a = (double)at * std::pow(g.rope_base, -(double)j / pairs);
+          const size_t i = (size_t)at * pairs + j;
+          wide[i] = make_double2(std::cos(a), std::sin(a));
+          tab[i] = make_float2((float)wide[i].x, (float)wide[i].y);
+        }
+    };
+    fill(g.gh, g.n_h, th64, th);
+    fill(g.gw, g.n_w, tw64, tw);
     bool ok = hipGetDevice(&c->device) == hipSuccess;
     ok = ok && hipDeviceGetAttribute(&c->n_cus, hipDeviceAttributeMultiprocessorCount, c->device) == hipSuccess && c->n_cus > 0;
     ok = ok && hipMalloc((void**)&c->d_inv_freq_t, inv_t.size() * sizeof(double)) == hipSuccess;
     ok = ok && hipMalloc((void**)&c->d_tab_h, th.size() * sizeof(float2)) == hipSuccess;
     ok = ok && hipMalloc((void**)&c->d_tab_w, tw.size() * sizeof(float2)) == hipSuccess;
+    ok = ok && hipMalloc((void**)&c->d_tab_h64, th64.size() * sizeof(double2)) == hipSuccess;
+    ok = ok && hipMalloc((void**)&c->d_tab_w64, tw64.size() * sizeof(double2)) == hipSuccess;
     ok = ok && hipMemcpy(c->d_inv_freq_t, inv_t.data(), inv_t.size() * sizeof(double), hipMemcpyHostToDevice) == hipSuccess;
     ok = ok && hipMemcpy(c->d_tab_h, th.data(), th.size() * sizeof(float2), hipMemcpyHostToDevice) == hipSuccess;
     ok = ok && hipMemcpy(c->d_tab_w, tw.data(), tw.size() * sizeof(float2), hipMemcpyHostToDevice) == hipSuccess;
+    ok = ok && hipMemcpy(c->d_tab_h64, th64.data(), th64.size() * sizeof(double2), hipMemcpyHostToDevice) == hipSuccess;
+    ok = ok && hipMemcpy(c->d_tab_w64, tw64.data(), tw64.size() * sizeof(double2), hipMemcpyHostToDevice) == hipSuccess;
     if (!ok) {
       (void)hipGetLastError();
       astro_kvcache_destroy(c);
@@ -434,6 +444,8 @@ int astro_kvcache_destroy(astro_kvcache_t* cache) {
   if (cache->d_inv_freq_t && hipFree(cache->d_inv_freq_t) != hipSuccess) rc = ASTRO_ERR_HIP;
   if (cache->d_tab_h && hipFree(cache->d_tab_h) != hipSuccess) rc = ASTRO_ERR_HIP;
   if (cache->d_tab_w && hipFree(cache->d_tab_w) != hipSuccess) rc = ASTRO_ERR_HIP;
+  if (cache->d_tab_h64 && hipFree(cache->d_tab_h64) != hipSuccess) rc = ASTRO_ERR_HIP;
+  if (cache->d_tab_w64 && hipFree(cache->d_tab_w64) != hipSuccess) rc = ASTRO_ERR_HIP;
   delete cache;
   return rc;
 }

@@ -38,6 +38,8 @@ struct DevGeom {
   const double* inv_freq_t;  // [n_t]  frequency of each temporal pair (fp64)
   const float2* tab_h;       // [gh][n_h] (cos, sin) of row position * frequency
   const float2* tab_w;       // [gw][n_w] (cos, sin) of column position * frequency
+  const double2* tab_h64;    // both before they are rounded, for the keys that a bf16 append caches (cached_pair)
+  const double2* tab_w64;
 };
 
 // Where a rotated / copied chunk tensor goes: head-major rows [B][H][rows_per_head][D];

@@ -2,6 +2,7 @@
 // Used by the KV append (keys rotated into their ring slot, values copied; Sec. 3.2)
 // and by the attention pre-pass (queries and chunk keys rotated into the workspace).
 // HBM-bound: every element is read once and written once, 16 bytes per lane.
+#include "cached_key.hpp"
 #include "kernels.hpp"
 #include "ring_state.hpp"
 
@@ -37,6 +38,56 @@ __device__ __forceinline__ float2 pair_cs(const float2* tab, const DevGeom& g, i
   return pair < nb ? tab[pair] : g.tab_w[w * g.n_w + (pair - nb)];
 }
 
+// An append of bf16 frames: keys turned into their ring slots (as cached_key.hpp says), values copied.  Loads ahead as in the kernel below.
+// grid: x = n_frames * gh (frame in chunk, row), y = head, z = stream
+template <int D>
+__global__ void __launch_bounds__(kThreads) append_rope_kernel(DevGeom g, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                                                               __bf16* __restrict__ k_cache, __bf16* __restrict__ v_cache, int n_frames,
+                                                               StreamInts first_frame, StreamInts next_n) {
+  constexpr int CPR = D / 8, kRows = kThreads / CPR, kUnroll = 4;
+  __shared__ double2 tab[D / 2];
+  const int fi = blockIdx.x / g.gh, row = blockIdx.x - fi * g.gh, h = blockIdx.y, b = blockIdx.z, t = threadIdx.x;
+  const bool rope = g.n_t + g.n_h + g.n_w != 0;
+  const int c = t % CPR, w0 = t / CPR, stride = g.H * D;  // a row's offsets fit 32 bits: 4096 columns, 1024 heads
+  const int slot = slot_of_frame_number((int64_t)next_n.v[b] + fi, g.C, g.S);
+  const int64_t in = ((((int64_t)b * n_frames + fi) * g.T + (int64_t)row * g.gw) * g.H + h) * D + c * 8;
+  const int64_t out = (((int64_t)b * g.H + h) * g.C * g.T + (int64_t)slot * g.T + (int64_t)row * g.gw) * D + c * 8;
+  const __bf16 *k_from = k + in, *v_from = v + in;
+  __bf16 *k_to = k_cache + out, *v_to = v_cache + out;
+  for (int base = 0; base < g.gw; base += kUnroll * kRows) {
+    bf16x8 x[kUnroll], y[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int w = base + u * kRows + w0;
+      if (w < g.gw) {
+        x[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(k_from + w * stride));
+        y[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(v_from + w * stride));
+      }
+    }
+    ExactAngles at;
+    auto angles = [&](int w) __attribute__((always_inline)) { at.load(g, tab, row, w < g.gw ? w : g.gw - 1, c * 4); };
+    if (rope) {
+      if (base == 0) {  // under the loads
+        exact_temporal(g, tab, first_frame.v[b] + fi);
+        __syncthreads();
+      }
+      angles(base + w0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int w = base + u * kRows + w0;
+      if (w >= g.gw) continue;
+      if (rope) {
+        x[u] = cached_key8(x[u], at);
+        if (u + 1 < kUnroll) angles(w + kRows);  // before the stores: a wait for them would be a wait for the stores as well
+      }
+      __builtin_nontemporal_store(x[u], reinterpret_cast<bf16x8*>(k_to + w * D));
+      __builtin_nontemporal_store(y[u], reinterpret_cast<bf16x8*>(v_to + w * D));
+    }
+  }
+}
+
+// The pre-pass, and the fp32 path's append.
 // grid: x = n_frames * gh (frame in chunk, row), y = head, z = stream
 template <typename Elem, bool kRotateB>
 __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const Elem* __restrict__ a_in,
@@ -57,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const
   if constexpr (sizeof(Elem) == 2) {
     // kUnroll chunks of each tensor per lane and trip: all their loads are issued before the
     // first is used (2 * kUnroll 16-byte loads in flight per lane), and every element is
-    // touched once, so the loads (and the append's stores) bypass the caches' keep-for-reuse policy.
+    // touched once, so the loads bypass the caches' keep-for-reuse policy.
     // Measured on a plain copy of 1 GiB: 6.0 TB/s this way against 4.5 TB/s one chunk at a time.
     // The first trip's loads are issued before the block's (cos, sin) table is built, so the
     // fp64 sincos of the temporal pairs runs under their latency.
@@ -94,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const
             const float a0 = (float)xa[u][2 * v], a1 = (float)xa[u][2 * v + 1];
             xa[u][2 * v] = (__bf16)((a0 * cs.x - a1 * cs.y) * a_scale);
             xa[u][2 * v + 1] = (__bf16)((a0 * cs.y + a1 * cs.x) * a_scale);
-            if (kRotateB) {
+            if constexpr (kRotateB) {
               const float b0 = (float)xb[u][2 * v], b1 = (float)xb[u][2 * v + 1];
               xb[u][2 * v] = (__bf16)(b0 * cs.x - b1 * cs.y);
               xb[u][2 * v + 1] = (__bf16)(b0 * cs.y + b1 * cs.x);
@@ -105,13 +156,9 @@ __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const
 #pragma unroll
           for (int v = 0; v < 8; ++v) xa[u][v] = (__bf16)((float)xa[u][v] * a_scale);
         }
-        if constexpr (kRotateB) {  // staged Q~, K~: read again at once by the attention launch
-          *reinterpret_cast<bf16x8*>(a_out + out_off) = xa[u];
-          *reinterpret_cast<bf16x8*>(b_out + out_off) = xb[u];
-        } else {
-          __builtin_nontemporal_store(xa[u], reinterpret_cast<bf16x8*>(a_out + out_off));
-          __builtin_nontemporal_store(xb[u], reinterpret_cast<bf16x8*>(b_out + out_off));
-        }
+        // staged Q~, K~: read again at once by the attention launch
+        *reinterpret_cast<bf16x8*>(a_out + out_off) = xa[u];
+        *reinterpret_cast<bf16x8*>(b_out + out_off) = xb[u];
       }
     }
     return;
@@ -190,23 +237,35 @@ __global__ void __launch_bounds__(kThreads) rope_sink_rerotate_kernel(DevGeom g,
                                                                       StreamInts count) {
   constexpr int EPC = 16 / sizeof(Elem);
   typedef Elem Chunk __attribute__((ext_vector_type(EPC)));
-  __shared__ float2 tab[kMaxBlockPairs];
+  constexpr bool kCached = sizeof(Elem) == 2;
+  __shared__ std::conditional_t<kCached, double2, float2> tab[kMaxBlockPairs];
   const int s = blockIdx.x / g.gh, row = blockIdx.x % g.gh;
   const int h = blockIdx.y, b = blockIdx.z;
   if (s >= count.v[b]) return;  // whole block
-  fill_block_table(tab, g, first_pos.v[b] + s, row);
+  if constexpr (kCached) {
+    exact_temporal(g, tab, first_pos.v[b] + s);
+    __syncthreads();
+  } else {
+    fill_block_table(tab, g, first_pos.v[b] + s, row);
+  }
   const int cpr = g.D / EPC;
   const int64_t in_tok0 = ((int64_t)b * g.S + s) * g.T + (int64_t)row * g.gw;
   const int64_t out_row0 = ((int64_t)b * g.H + h) * ((int64_t)g.C * g.T) + (int64_t)s * g.T + (int64_t)row * g.gw;
   for (int idx = threadIdx.x; idx < g.gw * cpr; idx += kThreads) {
     const int w = idx / cpr, c = idx % cpr;
     Chunk x = *reinterpret_cast<const Chunk*>(sink_raw + ((in_tok0 + w) * g.H + h) * g.D + c * EPC);
+    if constexpr (kCached) {
+      ExactAngles at;
+      at.load(g, tab, row, w, c * 4);
+      x = cached_key8(x, at);
+    } else {
 #pragma unroll
-    for (int v = 0; v < EPC / 2; ++v) {
-      const float2 cs = pair_cs(tab, g, w, c * (EPC / 2) + v);
-      const float x0 = (float)x[2 * v], x1 = (float)x[2 * v + 1];
-      x[2 * v] = (Elem)(x0 * cs.x - x1 * cs.y);
-      x[2 * v + 1] = (Elem)(x0 * cs.y + x1 * cs.x);
+      for (int v = 0; v < EPC / 2; ++v) {
+        const float2 cs = pair_cs(tab, g, w, c * (EPC / 2) + v);
+        const float x0 = (float)x[2 * v], x1 = (float)x[2 * v + 1];
+        x[2 * v] = (Elem)(x0 * cs.x - x1 * cs.y);
+        x[2 * v + 1] = (Elem)(x0 * cs.y + x1 * cs.x);
+      }
     }
     *reinterpret_cast<Chunk*>(k_cache + (out_row0 + w) * g.D + c * EPC) = x;
   }
@@ -225,9 +284,10 @@ hipError_t launch_rope_scatter(const DevGeom& g, int dtype, const void* a_in, co
     if (rotate_b)
       rope_scatter_kernel<__bf16, true><<<grid, block, 0, stream>>>(g, a, b, (__bf16*)dst.a, (__bf16*)dst.b,
                                                                    dst.rows_per_head, dst.ring, n_frames, first_frame, next_n, tab_t_out, a_scale);
+    else if (g.D == 128)
+      append_rope_kernel<128><<<grid, block, 0, stream>>>(g, a, b, (__bf16*)dst.a, (__bf16*)dst.b, n_frames, first_frame, next_n);
     else
-      rope_scatter_kernel<__bf16, false><<<grid, block, 0, stream>>>(g, a, b, (__bf16*)dst.a, (__bf16*)dst.b,
-                                                                    dst.rows_per_head, dst.ring, n_frames, first_frame, next_n, tab_t_out, a_scale);
+      append_rope_kernel<64><<<grid, block, 0, stream>>>(g, a, b, (__bf16*)dst.a, (__bf16*)dst.b, n_frames, first_frame, next_n);
   } else {
     auto a = static_cast<const float*>(a_in);
     auto b = static_cast<const float*>(b_in);

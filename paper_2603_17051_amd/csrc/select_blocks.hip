@@ -6,6 +6,7 @@
 // Sums and products are 64 bits: a selection is a set of integers, and in 32 bits its last member would depend on the
 // order of the sums.  (bf16 values have 8 bits, so their 64-bit sums over a block are as good as exact in any order.)
 // Means of what was handed in do not depend on positions: they stay right when sinks are rotated again.
+#include "cached_key.hpp"
 #include "kernels.hpp"
 #include "mfma_common.hpp"
 #include "ring_state.hpp"
@@ -46,11 +47,11 @@ __global__ void __launch_bounds__(kThreads) append_means_kernel(DevGeom g, const
                                                                 StreamInts first_frame, StreamInts next_n) {
   constexpr int CPR = D / 8, kRows = kThreads / CPR, kUnroll = 4;
   __shared__ double scratch[kThreads * 8];
-  __shared__ float2 tab_t[D / 2];
+  __shared__ double2 tab_t[D / 2];
   const int fi = blockIdx.x / frame_blocks, j = blockIdx.x - fi * frame_blocks, h = blockIdx.y, b = blockIdx.z, t = threadIdx.x;
   const int first = j * key_block, n = g.T - first < key_block ? g.T - first : key_block;
   const int slot = slot_of_frame_number((int64_t)next_n.v[b] + fi, g.C, g.S);
-  const int c = t % CPR, r0 = t / CPR, nb = g.n_t + g.n_h;
+  const int c = t % CPR, r0 = t / CPR;
   const bool rope = g.n_t + g.n_h + g.n_w != 0;
   const int64_t in0 = ((((int64_t)b * n_frames + fi) * g.T + first) * g.H + h) * D + c * 8, stride = (int64_t)g.H * D;
   const int64_t out0 = (((int64_t)b * g.H + h) * g.C * g.T + (int64_t)slot * g.T + first) * D + c * 8;
@@ -66,13 +67,15 @@ __global__ void __launch_bounds__(kThreads) append_means_kernel(DevGeom g, const
       }
     }
     if (rope && base == 0) {  // under the loads
-      if (t < g.n_t) {
-        double s, cs;
-        sincos((double)(first_frame.v[b] + fi) * g.inv_freq_t[t], &s, &cs);
-        tab_t[t] = make_float2((float)cs, (float)s);
-      }
+      exact_temporal(g, tab_t, first_frame.v[b] + fi);
       __syncthreads();
     }
+    ExactAngles at;
+    auto angles = [&](int r) __attribute__((always_inline)) {
+      const int tok = first + (r < n ? r : n - 1), row = tok / g.gw;
+      at.load(g, tab_t, row, tok - row * g.gw, c * 4);
+    };
+    if (rope) angles(base + r0);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int r = base + u * kRows + r0;
@@ -80,14 +83,8 @@ __global__ void __launch_bounds__(kThreads) append_means_kernel(DevGeom g, const
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += (double)(float)x[u][i];
       if (rope) {
-        const int tok = first + r, row = tok / g.gw, col = tok - row * g.gw;
-        float2 cs[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int pair = c * 4 + i;
-          cs[i] = pair < g.n_t ? tab_t[pair] : pair < nb ? g.tab_h[row * g.n_h + (pair - g.n_t)] : g.tab_w[col * g.n_w + (pair - nb)];
-        }
-        x[u] = rotate8(x[u], cs, 1.f);
+        x[u] = cached_key8(x[u], at);
+        if (u + 1 < kUnroll) angles(r + kRows);  // before the stores: a wait for them would be a wait for the stores as well
       }
       __builtin_nontemporal_store(x[u], reinterpret_cast<bf16x8*>(k_cache + out0 + r * D));
       __builtin_nontemporal_store(y[u], reinterpret_cast<bf16x8*>(v_cache + out0 + r * D));
