@@ -276,9 +276,10 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
 #pragma unroll
   for (int qs = 0; qs < QS; ++qs) {
     const float l_tot = sum_quarters(w.sum[qs]);
-    // a key range in which a query sees nothing reports zeros and a log-sum-exp of -1e30, weight 0 in the merge
-    const bool nothing = !(l_tot > 0.f);
-    const float inv = nothing ? 0.f : 1.f / l_tot, lse = nothing ? kNegBig : w.ref[qs] * kLn2 + __logf(l_tot);
+    // a key range in which a query sees nothing reports zeros and a log-sum-exp of -inf, weight 0 in the merge; a sum that is not a number
+    // stays one
+    const bool nothing = p.splits > 1 && l_tot == 0.f;
+    const float inv = nothing ? 0.f : 1.f / l_tot, lse = w.ref[qs] * kLn2 + __logf(l_tot);
     const int q = q_wave + 16 * qs + i16;
     if (q >= p.Nq) continue;
     const int64_t row = (((int64_t)b * p.Nq + q) * p.H + h) * D + 4 * g;
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(256) select_merge_kernel(SelectFwdParams p, ui
   if (row >= n_rows) return;
   const uint32_t c = threadIdx.x % CPR, bq = row / (uint32_t)p.H, b = bq / (uint32_t)p.Nq;
   const uint32_t lse_at = (b * p.H + (row - bq * p.H)) * p.Nq + (bq - b * p.Nq);
-  float m = kNegBig, l[kMaxSelectSplits];
+  float m = kNegBig, l[kMaxSelectSplits];  // (m: over no number; one that is none makes its weight none)
   f32x4 o[kMaxSelectSplits];
 #pragma unroll
   for (uint32_t s = 0; s < kMaxSelectSplits; ++s) {  // (the first part again for those that are not there: no branch between loads)
