@@ -87,17 +87,20 @@ struct SelectDqWave {
     return x;
   }
 
-  template <bool kChunk, bool kEdge>  // as in the forward
-  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest) {
+  template <bool kChunk, bool kCare>  // as in the forward
+  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring = false) {
     const char *ks = stage, *vs = stage + kSelectTile * D * 2, *lo = stage + 2 * kSelectTile * D * 2;
     f32x4 s[2][QS], dp[2][QS], start[2][QS];
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) start[kh][qs] = neg_lse2[qs];
-    scores_from_halves<D, QS, kChunk>(ks, lo, addr, qh, ql, start, s);
+    if constexpr (kCare)
+      scores_of_any<D, QS>(ks, lo, !ring, addr, qh, ql, start, s);
+    else
+      scores_from_halves<D, QS, kChunk>(ks, lo, addr, qh, ql, start, s);
     // keys that do not count get a score that makes P and dS exactly 0
-    if (kEdge || fewest < kSelectTile) {
+    if (kCare || fewest < kSelectTile) {
 #pragma unroll
       for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -125,11 +128,11 @@ struct SelectDqWave {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           s[kh][qs][r] = fast_exp2(s[kh][qs][r]);
-          if constexpr (kEdge) dp[kh][qs][r] = 16 * kh + 4 * g + r >= live[qs] ? 0.f : dp[kh][qs][r];
+          if constexpr (kCare) dp[kh][qs][r] = 16 * kh + 4 * g + r >= live[qs] ? 0.f : dp[kh][qs][r];
         }
     bf16x8 a[2][4], c[2][4];  // of dQ~'s columns, four at a time, so that products on one accumulator lie apart
-    if constexpr (!kEdge) read_quad<D>(ks, addr, 0, a[0]);
-    if constexpr (kChunk && !kEdge) read_quad<D>(lo, addr, 0, c[0]);
+    if constexpr (!kCare) read_quad<D>(ks, addr, 0, a[0]);
+    if constexpr (kChunk && !kCare) read_quad<D>(lo, addr, 0, c[0]);
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 hi[QS], small[QS];
 #pragma unroll
@@ -138,22 +141,23 @@ struct SelectDqWave {
       for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
-          const HalfPairs x = halves(f32x2{s[kh][qs][r] * dp[kh][qs][r], s[kh][qs][r + 1] * dp[kh][qs][r + 1]});
+          const f32x2 ds = {s[kh][qs][r] * dp[kh][qs][r], s[kh][qs][r + 1] * dp[kh][qs][r + 1]};
+          const HalfPairs x = kCare ? halves_of_any(ds) : halves(ds);
           hi[qs][4 * kh + r] = x.hi[0], hi[qs][4 * kh + r + 1] = x.hi[1];
           small[qs][4 * kh + r] = x.lo[0], small[qs][4 * kh + r + 1] = x.lo[1];
         }
-    if constexpr (kEdge) {
+    if constexpr (kCare) {
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs)
         each_bound(live[qs], [&](int bound, bool mine) __attribute__((always_inline)) {
-          const u32x4 mask = rows_between(g, 0, bound);
+          const u32x4 mask = rows_between(g, 0, bound), low_mask = rows_between(g, 0, ring ? 0 : bound);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) {
             const bf16x8 x = only(mask, read_cols16<D>(ks, addr.tr[dt], 0));
-            f32x4 to = mfma16(x, hi[qs], dq[dt][qs]);
-            to = mfma16(x, small[qs], to);
-            to = mfma16(only(mask, read_cols16<D>(lo, addr.tr[dt], 0)), hi[qs], to);
-            dq[dt][qs] = either(mine, to, dq[dt][qs]);
+            const f32x4 big = mfma16(x, hi[qs], dq[dt][qs]);
+            f32x4 to = mfma16(x, small[qs], big);
+            to = mfma16(only(low_mask, read_cols16<D>(lo, addr.tr[dt], 0)), hi[qs], to);
+            dq[dt][qs] = either(mine, with_small(big, to), dq[dt][qs]);
             __builtin_amdgcn_sched_barrier(0);
           }
         });
@@ -227,21 +231,22 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dq_kernel(SelectB
     __syncthreads();
   };
   begin();
-  auto step = [&](int t, auto chunk_c, auto edge_c) __attribute__((always_inline)) {
-    constexpr bool kChunk = decltype(chunk_c)::value, kEdge = decltype(edge_c)::value;
+  auto step = [&](int t, auto chunk_c, auto care_c) __attribute__((always_inline)) {
+    constexpr bool kChunk = decltype(chunk_c)::value, kCare = decltype(care_c)::value;
     const char* stage = Stages::of(lds, t - t_begin);
     if (t + kAhead < t_end) walk.issue(t + kAhead, walk.entry(t + kAhead), Stages::of(lds, t - t_begin + kAhead));
-    const int row0 = (t - walk.ring_tiles) * kSelectTile, fewest = kChunk ? vis_wave - row0 : walk.rows_of(t);
+    const bool ring = kCare ? t < walk.ring_tiles : !kChunk;
+    const int row0 = (t - walk.ring_tiles) * kSelectTile, fewest = ring ? walk.rows_of(t) : vis_wave - row0;
     int live[QS];
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       live[qs] = fewest;
-      if (kEdge || (kChunk && p.block_rows != 0 && fewest < kSelectTile)) {
+      if (!ring && (kCare || (p.block_rows != 0 && fewest < kSelectTile))) {
         const int q = q_wave + 16 * qs + (lane & 15);
         live[qs] = min(max(visible_chunk_rows(q < q_last ? q : q_last, p.Nq, p.block_rows) - row0, 0), kSelectTile);
       }
     }
-    w.template tile<kChunk, kEdge>(stage, live, fewest);
+    w.template tile<kChunk, kCare>(stage, live, fewest, ring);
     if (kAhead > 1)
       walk.wait_all_but(t + kAhead, t_end);
     else
@@ -253,12 +258,10 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dq_kernel(SelectB
     for (; t < t_end && t < walk.ring_tiles; ++t) step(t, std::false_type{}, std::false_type{});
     for (; t < t_end; ++t) step(t, std::true_type{}, std::false_type{});
   }
-  if (p.block_rows != 0 && walk.again(&tile_list, w.not_numbers_yet())) {
+  if (walk.again(&tile_list, w.not_numbers_yet())) {
     w.clear();
     begin();
-    int t = t_begin;
-    for (; t < t_end && t < walk.ring_tiles; ++t) step(t, std::false_type{}, std::false_type{});
-    for (; t < t_end; ++t) step(t, std::true_type{}, std::true_type{});
+    for (int t = t_begin; t < t_end; ++t) step(t, std::true_type{}, std::true_type{});
   }
 
   const bool rope = p.rot.n_t + p.rot.n_h + p.rot.n_w != 0;
@@ -376,8 +379,8 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     wait_vmem();
     __syncthreads();
   };
-  auto step = [&](int t, auto edge_c) __attribute__((always_inline)) {
-    constexpr bool kEdge = decltype(edge_c)::value;
+  auto step = [&](int t, auto care_c) __attribute__((always_inline)) {
+    constexpr bool kCare = decltype(care_c)::value;
     const char *qs = Stages::of(lds, t - t_begin), *dos = qs + kTileBytes, *lo = qs + 2 * kTileBytes;
     if (t + kAhead < t_end) issue(t + kAhead);
     take_term(t + kAhead);
@@ -388,12 +391,20 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
       start[qh][0] = *reinterpret_cast<const f32x4*>(&row_terms[0][16 * qh + 4 * g]);
       dp[qh] = *reinterpret_cast<const f32x4*>(&row_terms[1][16 * qh + 4 * g]);
     }
-    scores_from_halves<D, 1, true>(qs, lo, addr, kh, kl, start, s);
-    if (kEdge || t * kSelectTile < last_first) {
+    // of the tile's queries: this lane's key is a key of [from, to)
+    const int from = min(max(first - t * kSelectTile, 0), kSelectTile), to = min(p.Nq - t * kSelectTile, kSelectTile);
+    if constexpr (kCare)
+      scores_of_any<D, 1>(qs, lo, true, addr, kh, kl, start, s);
+    else
+      scores_from_halves<D, 1, true>(qs, lo, addr, kh, kl, start, s);
+    if (kCare || t * kSelectTile < last_first) {
 #pragma unroll
       for (int qh = 0; qh < 2; ++qh)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[qh][0][r] = t * kSelectTile + 16 * qh + 4 * g + r < first ? kNegBig : s[qh][0][r];
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * qh + 4 * g + r;
+          s[qh][0][r] = row < from || (kCare && row >= to) ? kNegBig : s[qh][0][r];
+        }
     }
     bf16x8 dor[KS][2];
 #pragma unroll
@@ -409,14 +420,17 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     for (int qh = 0; qh < 2; ++qh)
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[qh][0][r] = fast_exp2(s[qh][0][r]);
-    if constexpr (kEdge) {
+    if constexpr (kCare) {
 #pragma unroll
       for (int qh = 0; qh < 2; ++qh)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) dp[qh][r] = t * kSelectTile + 16 * qh + 4 * g + r < first ? 0.f : dp[qh][r];
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * qh + 4 * g + r;
+          dp[qh][r] = row < from || row >= to ? 0.f : dp[qh][r];
+        }
     }
     bf16x8 a[2][4], c[2][4];  // of the gradients' columns, four at a time, so that products on one accumulator lie apart
-    if constexpr (!kEdge) read_quad<D>(dos, addr, 0, a[0]);
+    if constexpr (!kCare) read_quad<D>(dos, addr, 0, a[0]);
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 p_hi, p_lo, ds_hi, ds_lo;
 #pragma unroll
@@ -424,7 +438,8 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
         const f32x2 pr = {s[qh][0][r], s[qh][0][r + 1]};
-        const HalfPairs x = halves(pr), y = halves(f32x2{pr[0] * dp[qh][r], pr[1] * dp[qh][r + 1]});
+        const f32x2 ds = {pr[0] * dp[qh][r], pr[1] * dp[qh][r + 1]};
+        const HalfPairs x = kCare ? halves_of_any(pr) : halves(pr), y = kCare ? halves_of_any(ds) : halves(ds);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           p_hi[4 * qh + r + i] = x.hi[i], p_lo[4 * qh + r + i] = x.lo[i];
@@ -433,15 +448,16 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
       }
     __builtin_amdgcn_sched_barrier(0);
     constexpr int kQuads = DT / 4;
-    if constexpr (kEdge) {
-      each_bound(min(max(first - t * kSelectTile, 0), kSelectTile), [&](int bound, bool mine) __attribute__((always_inline)) {
-        const u32x4 mask = rows_between(g, bound, kSelectTile);
+    if constexpr (kCare) {
+      each_bound(from, [&](int bound, bool mine) __attribute__((always_inline)) {
+        const u32x4 mask = rows_between(g, bound, to);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const bf16x8 x = only(mask, read_cols16<D>(dos, addr.tr[dt], 0)), y = only(mask, read_cols16<D>(qs, addr.tr[dt], 0));
-          const f32x4 to_v = mfma16(x, p_lo, mfma16(x, p_hi, dv[dt])), part = mfma16(y, ds_lo, mfma16(y, ds_hi, dk[dt]));
-          dv[dt] = either(mine, to_v, dv[dt]);
-          dk[dt] = either(mine, mfma16(only(mask, read_cols16<D>(lo, addr.tr[dt], 0)), ds_hi, part), dk[dt]);
+          const f32x4 big_v = mfma16(x, p_hi, dv[dt]), big_k = mfma16(y, ds_hi, dk[dt]);
+          dv[dt] = either(mine, with_small(big_v, mfma16(x, p_lo, big_v)), dv[dt]);
+          const f32x4 all_k = mfma16(only(mask, read_cols16<D>(lo, addr.tr[dt], 0)), ds_hi, mfma16(y, ds_lo, big_k));
+          dk[dt] = either(mine, with_small(big_k, all_k), dk[dt]);
           __builtin_amdgcn_sched_barrier(0);
         }
       });
@@ -489,7 +505,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     asm volatile("" : "+s"(t));  // (beside the second walk's the compiler counts this loop in vector registers: 3 % of the launch)
     step(t, std::false_type{});
   }
-  if (p.block_rows != 0) {  // (see each_bound)
+  {  // (see each_bound)
     bool not_numbers_yet = false;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) not_numbers_yet = not_numbers_yet || not_numbers(dk[dt]) || not_numbers(dv[dt]);

@@ -106,19 +106,23 @@ struct SelectFwdWave {
   }
 
   // One tile of 32 keys, of which the first live[qs] count for this lane's query qs (fewest, wave-uniform, for any of the wave).
-  // kEdge: the others may hold anything, else what they hold has to be finite.
-  template <bool kChunk, bool kEdge>
-  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest) {
+  // kCare: with care (see each_bound()), for tiles of both kinds (`ring`: which; a second instance of the careful code moved the registers
+  // of the backward's first walk, 1080 -> 1270 us); else what the tile holds has to be finite.
+  template <bool kChunk, bool kCare>
+  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring = false) {
     const char *vs = stage + kSelectTile * D * 2, *lo = stage + 2 * kSelectTile * D * 2;
     f32x4 s[2][QS], start[2][QS];  // the scores come out relative to the reference
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) start[kh][qs] = f32x4{-ref[qs], -ref[qs], -ref[qs], -ref[qs]};
-    scores_from_halves<D, QS, kChunk>(stage, lo, addr, qh, ql, start, s);
+    if constexpr (kCare)
+      scores_of_any<D, QS>(stage, lo, !ring, addr, qh, ql, start, s);
+    else
+      scores_from_halves<D, QS, kChunk>(stage, lo, addr, qh, ql, start, s);
     bf16x8 v[2][4];  // of the output's columns, four at a time: the first under the softmax
-    if constexpr (!kEdge) read_quad<D>(vs, addr, 0, v[0]);
-    if (kEdge || fewest < kSelectTile) {
+    if constexpr (!kCare) read_quad<D>(vs, addr, 0, v[0]);
+    if (kCare || fewest < kSelectTile) {
 #pragma unroll
       for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -156,7 +160,7 @@ struct SelectFwdWave {
     if (__builtin_expect(__any(look), 0)) move_reference(s, part, probabilities);
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) sum[qs] += part[qs];
-    if constexpr (kEdge) {
+    if constexpr (kCare) {
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs)
         each_bound(live[qs], [&](int bound, bool mine) __attribute__((always_inline)) {
@@ -241,21 +245,22 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
     __syncthreads();
   };
   begin();
-  auto step = [&](int t, auto chunk_c, auto edge_c) __attribute__((always_inline)) {
-    constexpr bool kChunk = decltype(chunk_c)::value, kEdge = decltype(edge_c)::value;
+  auto step = [&](int t, auto chunk_c, auto care_c) __attribute__((always_inline)) {
+    constexpr bool kChunk = decltype(chunk_c)::value, kCare = decltype(care_c)::value;
     const char* stage = Stages::of(lds, t - t_begin);
     if (t + kAhead < t_end) walk.issue(t + kAhead, walk.entry(t + kAhead), Stages::of(lds, t - t_begin + kAhead));
-    const int row0 = (t - walk.ring_tiles) * kSelectTile, fewest = kChunk ? vis_wave - row0 : walk.rows_of(t);
+    const bool ring = kCare ? t < walk.ring_tiles : !kChunk;
+    const int row0 = (t - walk.ring_tiles) * kSelectTile, fewest = ring ? walk.rows_of(t) : vis_wave - row0;
     int live[QS];
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       live[qs] = fewest;
-      if (kEdge || (kChunk && p.block_rows != 0 && fewest < kSelectTile)) {
+      if (!ring && (kCare || (p.block_rows != 0 && fewest < kSelectTile))) {
         const int q = q_wave + 16 * qs + i16;
         live[qs] = min(max(visible_chunk_rows(q < q_last ? q : q_last, p.Nq, p.block_rows) - row0, 0), kSelectTile);
       }
     }
-    w.template tile<kChunk, kEdge>(stage, live, fewest);
+    w.template tile<kChunk, kCare>(stage, live, fewest, ring);
     walk.wait_all_but(t + kAhead, t_end);
     __syncthreads();
   };
@@ -264,12 +269,10 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
     for (; t < t_end && t < walk.ring_tiles; ++t) step(t, std::false_type{}, std::false_type{});
     for (; t < t_end; ++t) step(t, std::true_type{}, std::false_type{});
   }
-  if (p.block_rows != 0 && walk.again(&tile_list, w.not_numbers_yet())) {
+  if (walk.again(&tile_list, w.not_numbers_yet())) {
     w.clear();
     begin();
-    int t = t_begin;
-    for (; t < t_end && t < walk.ring_tiles; ++t) step(t, std::false_type{}, std::false_type{});
-    for (; t < t_end; ++t) step(t, std::true_type{}, std::true_type{});
+    for (int t = t_begin; t < t_end; ++t) step(t, std::true_type{}, std::true_type{});
   }
 
   // normalise, write O [B, Nq, H, D] and LSE [B, H, Nq] (of this split's keys)

@@ -42,7 +42,8 @@ __global__ void __launch_bounds__(kThreads) select_stage_kernel(DevGeom g, const
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         const float a = (float)x[m][2 * v], e = (float)x[m][2 * v + 1], scale = m == 0 ? q_scale : 1.f;
-        const HalfPairs r = halves(f32x2{(a * cs.x - e * cs.y) * scale, (a * cs.y + e * cs.x) * scale});
+        const f32x2 turned = rope ? f32x2{a * cs.x - e * cs.y, a * cs.y + e * cs.x} : f32x2{a, e};  // (without: not through a product with 0)
+        const HalfPairs r = halves_of_any(turned * scale);
         hi[m][2 * v] = r.hi[0], hi[m][2 * v + 1] = r.hi[1];
         lo[m][2 * v] = r.lo[0], lo[m][2 * v + 1] = r.lo[1];
       }

@@ -164,6 +164,20 @@ __device__ __forceinline__ HalfPairs halves(f32x2 x) {
   return HalfPairs{hi, __builtin_convertvector(x - __builtin_convertvector(hi, f32x2), bf16x2)};
 }
 
+// The same where x may be infinite: no small half then, which would be inf - inf.
+__device__ __forceinline__ HalfPairs halves_of_any(f32x2 x) {
+  const bf16x2 hi = __builtin_convertvector(x, bf16x2);
+  const f32x2 big = __builtin_convertvector(hi, f32x2), rest = x - big;
+  return HalfPairs{hi, __builtin_convertvector(f32x2{__builtin_isfinite(big[0]) ? rest[0] : 0.f, __builtin_isfinite(big[1]) ? rest[1] : 0.f}, bf16x2)};
+}
+// of a sum without and with its products of small halves: the former where it is infinite or not a number (a small half has a sign of its own or is 0)
+__device__ __forceinline__ f32x4 with_small(const f32x4& without, const f32x4& with) {
+  f32x4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __builtin_isfinite(without[i]) ? with[i] : without[i];
+  return x;
+}
+
 // The scores of 16 rows of the other side in fp32 from halves: S = start + A (B_hi + B_lo)^T (+ A_lo B_hi^T), where A comes from an
 // LDS tile and B is held, N sub-blocks of 16 rows of it.  An MFMA takes its result's place in the next but one at the earliest:
 // products on one accumulator are kept four apart, for N = 1 by an accumulator of their own for the small ones.
@@ -220,6 +234,32 @@ __device__ __forceinline__ void scores_from_halves(const char* tile, const char*
     for (int kh = 0; kh < 2; ++kh) s[kh][0] += small[kh];
 }
 
+// The same, bit for bit, where the sums without small halves are numbers; where operands may be infinite.  with_low: whether there is an A_lo.
+template <int D, int N>
+__device__ __forceinline__ void scores_of_any(const char* tile, const char* low, bool with_low, const OperandAddr16<D>& addr, const bf16x8 (&hi)[N][D / 32],
+                                              const bf16x8 (&lo)[N][D / 32], const f32x4 (&start)[2][N], f32x4 (&s)[2][N]) {
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      f32x4 big = start[kh][n], all = big, small = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < D / 32; ++st) {
+        const bf16x8 a = read_rows16<D>(tile, addr.row[st], 16 * kh);
+        bf16x8 c{};
+        if (with_low) c = read_rows16<D>(low, addr.row[st], 16 * kh);
+        big = mfma16(a, hi[n][st], big);
+        if constexpr (N == 1) {  // in the order of the products above
+          small = mfma16(c, hi[n][st], mfma16(a, lo[n][st], small));
+        } else {
+          all = mfma16(c, hi[n][st], mfma16(a, lo[n][st], mfma16(a, hi[n][st], all)));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      s[kh][n] = with_small(big, N == 1 ? big + small : all);
+    }
+}
+
 // Operands of the products that contract over a tile's 32 rows: columns 16 (4 quad) .. 16 (4 quad + 3) + 15 of it.
 template <int D>
 __device__ __forceinline__ void read_quad(const char* tile, const OperandAddr16<D>& addr, int quad, bf16x8 (&x)[4]) {
@@ -227,10 +267,11 @@ __device__ __forceinline__ void read_quad(const char* tile, const OperandAddr16<
   for (int i = 0; i < 4; ++i) x[i] = read_cols16<D>(tile, addr.tr[4 * quad + i], 0);
 }
 
-// Tiles that a causal block ends in.  A probability of 0 does not keep a row out of a matrix product whose element there is
-// infinite or not a number: 0 * inf.  A workgroup whose result is not a number therefore walks again, and such tiles go through the
-// products once for every distinct bound of a wave's lanes, with the rows behind the bound (or before it) as zeros, and
-// a lane takes the result of its own.  Done so at once, the passes at frames of 391 rows of D = 64 took a quarter to a half longer.
+// Values that are not finite.  A probability of 0 does not keep a row that a query does not see (behind the end of a causal block) out of a
+// matrix product whose element there is infinite or not a number: 0 * inf.  And products of small halves turn an infinite sum into inf - inf.  A
+// workgroup whose result is not a number therefore walks again, with care: tiles go through the products once for every distinct
+// bound of a wave's lanes, with the rows behind the bound (or before it) as zeros, a lane takes the result of its own, and sums
+// that are infinite without small halves stay as they are.  Done so at once, the passes at frames of 391 rows of D = 64 took a quarter to a half longer.
 template <typename F>
 __device__ __forceinline__ void each_bound(int bound, F f) {
   uint64_t left = ~0ull;
