@@ -638,6 +638,8 @@ def astro_kvcache_fork(dst: KVCache, src: KVCache, source, stream=None) -> None:
     source = [operator.index(s) for s in source]
     if len(source) != dst.desc.batch:
         raise ValueError(f"source: expected {dst.desc.batch} entries, one for each stream of dst, got {len(source)}")
+    if not all(-1 <= s < src.desc.batch for s in source):  # (an array of 32 bits takes any, modulo 2^32)
+        raise AstroError(ASTRO_ERR_INVALID_ARG, "astro_kvcache_fork")
     _check(_lib.astro_kvcache_fork(dst.handle, src.handle, (c_int32 * len(source))(*source),
                                    c_void_p(None) if dst.k_storage is None else _cache_stream(dst, stream)), "astro_kvcache_fork")
 
