@@ -169,6 +169,14 @@ def _check(code: int, where: str) -> None:
         raise AstroError(code, where)
 
 
+def _int32(x, where: str) -> int:
+    """ctypes hands an int that 32 bits do not hold over modulo 2^32."""
+    x = operator.index(x)
+    if not -1 << 31 <= x < 1 << 31:
+        raise AstroError(ASTRO_ERR_INVALID_ARG, where)
+    return x
+
+
 def _ptr(t) -> c_void_p:
     return c_void_p(None if t is None else t.data_ptr())
 
@@ -208,7 +216,7 @@ def astro_kvcache_sink_bytes(desc: astro_kvcache_desc_t) -> int:
 
 def astro_kvcache_mean_bytes(desc: astro_kvcache_desc_t, key_block: int) -> int:
     n = c_size_t(0)
-    _check(_lib.astro_kvcache_mean_bytes(byref(desc), key_block, byref(n)), "astro_kvcache_mean_bytes")
+    _check(_lib.astro_kvcache_mean_bytes(byref(desc), _int32(key_block, "astro_kvcache_mean_bytes"), byref(n)), "astro_kvcache_mean_bytes")
     return n.value
 
 
@@ -259,6 +267,7 @@ def astro_kvcache_create(batch, heads, head_dim, grid_h, grid_w, capacity_frames
                          device="cuda:0", block_frames=0, window_relative=False, reuse_staged=False, key_block=0) -> KVCache:
     """Allocate the K/V storage with torch (unless host_only) and create the handle.  key_block (32, 64, 128 or 256):
     keep the means of blocks of that many keys, which the calls over selected blocks need."""
+    key_block = _int32(key_block or 0, "astro_kvcache_create")
     flags = ((ASTRO_FLAG_HOST_ONLY if host_only else 0) | (ASTRO_FLAG_WINDOW_RELATIVE if window_relative else 0)
              | (ASTRO_FLAG_REUSE_STAGED if reuse_staged else 0))
     desc = make_desc(batch, heads, head_dim, grid_h, grid_w, capacity_frames, sink_frames, max_chunk_frames,
@@ -690,7 +699,8 @@ def astro_select_blocks(cache: KVCache, q, n_frames: int, n_select: int, query_b
 
 def astro_select_attn_workspace_bytes(cache: KVCache, n_frames: int, group: int = 1):
     f, b = c_size_t(0), c_size_t(0)
-    _check(_lib.astro_select_attn_workspace_bytes(cache.handle, n_frames, group, byref(f), byref(b)), "astro_select_attn_workspace_bytes")
+    where = "astro_select_attn_workspace_bytes"
+    _check(_lib.astro_select_attn_workspace_bytes(cache.handle, _int32(n_frames, where), _int32(group, where), byref(f), byref(b)), where)
     return f.value, b.value
 
 
