@@ -680,7 +680,8 @@ def astro_select_blocks(cache: KVCache, q, n_frames: int, n_select: int, query_b
     given = blocks is not None
     if n_select * 32 > ASTRO_MAX_SELECT_ROWS:
         raise AstroError(ASTRO_ERR_UNSUPPORTED, "astro_select_blocks")
-    if not given and n_select > 0 and n_frames > 0 and group > 0:
+    # nothing is allocated for sizes that the library refuses
+    if not given and n_select > 0 and 0 < n_frames <= cache.desc.max_chunk_frames and 0 < group * cache.desc.batch <= ASTRO_MAX_BATCH:
         blocks = torch.empty(_list_shape(cache, n_frames, n_select, query_block, group), dtype=torch.int32, device=q.device)
     if stream is None and blocks is not None and (not given or blocks.shape[-1] == n_select):
         code = _native.select(cache.handle, cache._native_dims, cache.k_storage, n_frames, group, query_block, blocks, q)

@@ -15,3 +15,13 @@ def test_sizes_beyond_32_bits_are_refused(off):
         with pytest.raises(A.AstroError) as e:
             call()
         assert e.value.code == binding.ASTRO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("frames,group", [(3, 1), (1 << 40, 1), (1, 33), (2, 1 << 40), (0, 1), (1, 0), (-1, 1), (1, -1)])
+def test_nothing_is_allocated_for_a_call_that_is_refused(frames, group, monkeypatch):
+    import torch
+    cache = A.astro_kvcache_create(*SIZES, host_only=True, key_block=32)
+    q = torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("allocated"))
+    with pytest.raises((ValueError, A.AstroError)):
+        A.astro_select_blocks(cache, q, frames, 2, 64, group)
