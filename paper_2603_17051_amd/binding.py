@@ -233,6 +233,7 @@ class KVCache:
         self.k_means = k_means  # fp32 [B, H, C * blocks of a frame, D]
         self._workspace = None
         self._select_bytes = {}  # workspace of the calls over selected blocks, by chunk frames and group
+        self._select_spaces = {}  # and one for every stream that such calls were made on
         # the desc as plain values: every call checks its tensors against them
         self._dims = (desc.batch, desc.grid_h * desc.grid_w, desc.heads, desc.head_dim)
         self._torch_dtype = torch.bfloat16 if desc.dtype == ASTRO_BF16 else torch.float32
@@ -705,22 +706,39 @@ def astro_select_attn_workspace_bytes(cache: KVCache, n_frames: int, group: int 
     return f.value, b.value
 
 
-def _select_workspace(cache: KVCache, n_frames: int, group: int, backward: bool) -> torch.Tensor:
+def _select_bytes(cache: KVCache, n_frames: int, group: int):
     key = (n_frames, group)
     if key not in cache._select_bytes:
         cache._select_bytes[key] = astro_select_attn_workspace_bytes(cache, n_frames, group)
-    return cache.workspace(cache._select_bytes[key][backward], cache.k_storage.device)
+    return cache._select_bytes[key]
+
+
+def _select_workspace(cache: KVCache, nbytes: int, stream) -> torch.Tensor:
+    """The workspace of a call that was given none: kept for the stream the call goes to, since calls on others may run at the same
+    time; of a call that is captured, the graph's own."""
+    device = cache.k_storage.device
+    if stream is not None:  # memory belongs to the stream that it is allocated on
+        with torch.cuda.stream(stream):
+            return _select_workspace(cache, nbytes, None)
+    handle = _cache_stream(cache, None).value or 0
+    if handle and torch.cuda.is_current_stream_capturing():  # (the default stream cannot be)
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    space = cache._select_spaces.get(handle)
+    if space is None or space.numel() < nbytes:
+        space = cache._select_spaces[handle] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    return space
 
 
 def astro_select_attn_fwd(cache: KVCache, q, k_chunk, v_chunk, blocks, n_frames: int, query_block: int = 128, group: int = 1, out=None,
                           lse=None, workspace=None, stream=None):
     """Attention over the listed blocks of the cache (lists as astro_select_blocks returns them) and the chunk's own keys.
-    Returns (out [B*group, Nq, H, D], lse [B*group, H, Nq] fp32)."""
+    Without a workspace the cache keeps one for each stream.  Returns (out [B*group, Nq, H, D], lse [B*group, H, Nq] fp32)."""
     _check_device(cache, q=q)
     batch, tokens, heads, _ = cache._dims
     rows = (batch * group, heads, n_frames * tokens)
+    nbytes = _select_bytes(cache, n_frames, group)[0]
     if workspace is None:
-        workspace = _select_workspace(cache, n_frames, group, False)
+        workspace = _select_workspace(cache, nbytes, stream)
     out = torch.empty_like(q) if out is None else out
     lse = torch.empty(rows, dtype=torch.float32, device=q.device) if lse is None else lse
     if stream is None:
@@ -746,8 +764,9 @@ def astro_select_attn_bwd(cache: KVCache, q, k_chunk, v_chunk, out, lse, dout, b
                           group: int = 1, dq=None, dk_chunk=None, dv_chunk=None, workspace=None, stream=None):
     """Backward of astro_select_attn_fwd for fixed lists.  Returns fp32 (dq, dk_chunk, dv_chunk), each [B*group, Nq, H, D]."""
     _check_device(cache, q=q)
+    nbytes = _select_bytes(cache, n_frames, group)[1]
     if workspace is None:
-        workspace = _select_workspace(cache, n_frames, group, True)
+        workspace = _select_workspace(cache, nbytes, stream)
     mk = lambda: torch.empty(q.shape, dtype=torch.float32, device=q.device)
     dq = mk() if dq is None else dq
     dk_chunk = mk() if dk_chunk is None else dk_chunk
