@@ -261,8 +261,8 @@ int astro_kvcache_fork(astro_kvcache_t *dst, const astro_kvcache_t *src, const i
 int astro_kvcache_mean_bytes(const astro_kvcache_desc_t *desc, int32_t key_block, size_t *bytes);
 
 /* Keep block means from now on: every append also writes the means of its frames' blocks to `means` (device,
- * 16-byte aligned, used until destroy; ignored by ASTRO_FLAG_HOST_ONLY handles).  All streams have to be empty
- * (ASTRO_ERR_BAD_STATE).  May be called again, also with another key_block. */
+ * 16-byte aligned, apart from the cache's storages, used until destroy; ignored by ASTRO_FLAG_HOST_ONLY handles).  All
+ * streams have to be empty (ASTRO_ERR_BAD_STATE).  May be called again, also with another key_block. */
 int astro_kvcache_keep_means(astro_kvcache_t *cache, int32_t key_block, float *means);
 
 /* For every group of queries and head the n_select (>= 1) resident blocks with the largest
@@ -270,7 +270,9 @@ int astro_kvcache_keep_means(astro_kvcache_t *cache, int32_t key_block, float *m
  * both as they were handed in, before rotation, means rounded to fp32, the product summed in 64 bits and rounded to fp32 (NaN counts as
  * -inf, ties go to the lower number).  blocks: lists as above, ascending, -1 behind the last where fewer blocks are resident.
  * q: device, [B*group, n_frames*T, H, D] of the cache dtype, un-rotated, 16-byte aligned; group as in astro_group_attn_fwd.
- * ASTRO_ERR_BAD_STATE without block means; ASTRO_ERR_UNSUPPORTED if C*nb exceeds ASTRO_MAX_SELECT_BLOCKS.
+ * blocks must not overlap q or anything that the cache keeps (ASTRO_ERR_INVALID_ARG).
+ * ASTRO_ERR_BAD_STATE without block means; ASTRO_ERR_UNSUPPORTED if C*nb exceeds ASTRO_MAX_SELECT_BLOCKS, or if lists of n_select entries are
+ * longer than the calls below take (ASTRO_MAX_SELECT_ROWS).
  * Allocates and synchronises nothing; needs no workspace. */
 int astro_select_blocks(const astro_kvcache_t *cache, const void *q, int32_t n_frames, int32_t group, int32_t query_block,
                         int32_t n_select, int32_t *blocks, void *hip_stream);
@@ -284,7 +286,7 @@ int astro_select_attn_workspace_bytes(const astro_kvcache_t *cache, int32_t n_fr
  * The causal mask inside the chunk, layouts, dtypes, workspace rules and errors are those of astro_group_attn_fwd, with
  * 16-byte aligned tensors.  n_select * (tiles of 32 rows of a block) * 32 <= ASTRO_MAX_SELECT_ROWS, else
  * ASTRO_ERR_UNSUPPORTED.  A row of the ring or the chunk that a query does not attend to leaves that query's results as they are, also
- * where it is not finite.  Outputs that overlap each other, an input or the workspace: ASTRO_ERR_INVALID_ARG.
+ * where it is not finite.  Outputs and workspace that overlap each other, an input or anything that the cache keeps: ASTRO_ERR_INVALID_ARG.
  * Needs a key_block (astro_kvcache_keep_means), else ASTRO_ERR_BAD_STATE; the lists may come from anywhere. */
 int astro_select_attn_fwd(astro_kvcache_t *cache, const void *q, const void *k_chunk, const void *v_chunk, int32_t n_frames,
                           int32_t group, const int32_t *blocks, int32_t query_block, int32_t n_select, void *out, float *lse,

@@ -162,6 +162,20 @@ bool overlap(const Span& a, const Span& b) {
   return x < y + b.bytes && y < x + a.bytes;
 }
 
+size_t mean_bytes(const RingGeometry& g, int key_block) {
+  return (size_t)g.B * g.H * g.C * ((g.T + key_block - 1) / key_block) * g.D * sizeof(float);
+}
+
+// Whether a buffer shares bytes with the rows that the cache keeps, or with anything that it keeps.
+bool over_rows(const astro_kvcache* c, const Span& s) {
+  const RingGeometry& g = c->geo;
+  return overlap(s, {c->k_storage, g.storage_bytes()}) || overlap(s, {c->v_storage, g.storage_bytes()}) ||
+         overlap(s, {c->k_sink_storage, g.sink_bytes()});
+}
+bool over_cache(const astro_kvcache* c, const Span& s) {
+  return over_rows(c, s) || (c->k_means && overlap(s, {c->k_means, mean_bytes(c->geo, c->key_block)}));
+}
+
 // Whether dK or dV of a bf16 backward shares bytes with the other, with dQ or with what only the query side
 // reads.  The two plain launches put up with that: the first reads all of these and writes dQ, the second
 // writes dK and dV (one buffer for gradients that are not wanted, gradients over an output that is
@@ -312,14 +326,16 @@ struct SelectSpans {
       for (const Tensor& s : *l)
         if (!s.at || ((uintptr_t)s.at & (s.words ? 3 : 15))) return ASTRO_ERR_INVALID_ARG;
     if (!workspace || have < need || ((uintptr_t)workspace & 255)) return ASTRO_ERR_WORKSPACE;
-    const RingGeometry& g = cache->geo;
+    const Span space{workspace, need};
+    if (over_cache(cache, space)) return ASTRO_ERR_INVALID_ARG;
+    for (const Tensor& i : in)
+      if (overlap(i, space)) return ASTRO_ERR_INVALID_ARG;
     for (const Tensor* s = out.begin(); s != out.end(); ++s) {
       for (const Tensor* o = out.begin(); o != s; ++o)
         if (overlap(*s, *o)) return ASTRO_ERR_INVALID_ARG;
       for (const Tensor& i : in)
         if (overlap(*s, i)) return ASTRO_ERR_INVALID_ARG;
-      for (const Span& i : {Span{workspace, need}, Span{cache->k_storage, g.storage_bytes()}, Span{cache->v_storage, g.storage_bytes()}})
-        if (overlap(*s, i)) return ASTRO_ERR_INVALID_ARG;
+      if (overlap(*s, space) || over_cache(cache, *s)) return ASTRO_ERR_INVALID_ARG;
     }
     return ASTRO_OK;
   }
@@ -730,7 +746,7 @@ int astro_kvcache_mean_bytes(const astro_kvcache_desc_t* desc, int32_t key_block
   RingGeometry g;
   const int rc = validate_desc(&d, &g);
   if (rc != ASTRO_OK) return rc;
-  *bytes = (size_t)g.B * g.H * g.C * ((g.T + key_block - 1) / key_block) * g.D * sizeof(float);
+  *bytes = mean_bytes(g, key_block);
   return ASTRO_OK;
 }
 
@@ -739,6 +755,7 @@ int astro_kvcache_keep_means(astro_kvcache_t* cache, int32_t key_block, float* m
   if (!cache->geo.host_only && (!means || ((uintptr_t)means & 15))) return ASTRO_ERR_INVALID_ARG;
   for (int b = 0; b < cache->geo.B; ++b)
     if (cache->tables.next_n(b) != 0) return ASTRO_ERR_BAD_STATE;
+  if (!cache->geo.host_only && over_rows(cache, {means, mean_bytes(cache->geo, key_block)})) return ASTRO_ERR_INVALID_ARG;
   cache->key_block = key_block;
   cache->k_means = means;
   return ASTRO_OK;
@@ -752,7 +769,8 @@ int astro_select_blocks(const astro_kvcache_t* cache, const void* q, int32_t n_f
   if (!q || ((uintptr_t)q & 15) || !blocks || ((uintptr_t)blocks & 3)) return ASTRO_ERR_INVALID_ARG;
   if ((int64_t)g.C * cache->frame_blocks() > ASTRO_MAX_SELECT_BLOCKS) return ASTRO_ERR_UNSUPPORTED;
   const size_t tokens = (size_t)g.B * group * g.H * n_frames * g.T, lists = (size_t)g.B * group * g.H * blocks_of(n_frames * g.T, query_block);
-  if (overlap({blocks, lists * n_select * sizeof(int32_t)}, {q, tokens * g.D * g.elem_bytes()})) return ASTRO_ERR_INVALID_ARG;
+  const Span to{blocks, lists * n_select * sizeof(int32_t)};
+  if (overlap(to, {q, tokens * g.D * g.elem_bytes()}) || over_cache(cache, to)) return ASTRO_ERR_INVALID_ARG;
   const OnDevice on(cache->device);
   if (!on.ok()) return ASTRO_ERR_HIP;
   StreamInts resident;
