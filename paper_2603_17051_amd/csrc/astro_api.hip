@@ -753,6 +753,7 @@ int astro_kvcache_mean_bytes(const astro_kvcache_desc_t* desc, int32_t key_block
 int astro_kvcache_keep_means(astro_kvcache_t* cache, int32_t key_block, float* means) {
   if (!cache || !is_key_block(key_block)) return ASTRO_ERR_INVALID_ARG;
   if (!cache->geo.host_only && (!means || ((uintptr_t)means & 15))) return ASTRO_ERR_INVALID_ARG;
+  if (cache->ring_undefined) return ASTRO_ERR_BAD_STATE;
   for (int b = 0; b < cache->geo.B; ++b)
     if (cache->tables.next_n(b) != 0) return ASTRO_ERR_BAD_STATE;
   if (!cache->geo.host_only && over_rows(cache, {means, mean_bytes(cache->geo, key_block)})) return ASTRO_ERR_INVALID_ARG;

@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 
-@pytest.mark.parametrize("name", ["overlaps"])
+@pytest.mark.parametrize("name", ["overlaps", "undefined"])
 def test_on_the_host(name, tmp_path, repo_root):
     exe = str(tmp_path / name)
     include = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("hipcc") or "/opt/rocm/bin/hipcc"))), "include")
