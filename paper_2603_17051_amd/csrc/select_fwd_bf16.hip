@@ -388,7 +388,7 @@ hipError_t launch_select_fwd_bf16(const DevGeom& g, const AttnOperands& op, cons
   const bool wide = lists.query_block % 128 == 0;
   if (g.D == 128)
     return wide ? launch<128, 2, 2>(g, op, staged, lists, out, lse, parts, stream) : launch<128, 1, 2>(g, op, staged, lists, out, lse, parts, stream);
-  return wide ? launch<64, 2, 3>(g, op, staged, lists, out, lse, parts, stream) : launch<64, 1, 4>(g, op, staged, lists, out, lse, parts, stream);
+  return wide ? launch<64, 2, 3>(g, op, staged, lists, out, lse, parts, stream) : launch<64, 1, 3>(g, op, staged, lists, out, lse, parts, stream);
 }
 
 }  // namespace astro
