@@ -309,9 +309,9 @@ __global__ void __launch_bounds__(256) select_dq_merge_kernel(SelectBwdParams p,
 }
 
 // ---- key side: 16 chunk keys of a wave, lane (i, g) owns key i; tiles of 32 queries -----------------------------------------
-template <int D, int kStages, int OCC>
+template <int D, int OCC>
 __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(SelectBwdParams p) {
-  constexpr int KS = D / 32, DT = D / 16, kAhead = kStages - 1, kKeys = kWaves * 16;
+  constexpr int KS = D / 32, DT = D / 16, kStages = 2, kAhead = kStages - 1, kKeys = kWaves * 16;
   using Stream = SharedStream<D, kWaves>;
   using Stages = SelectStages<D, kWaves, kStages>;
   constexpr int kTileBytes = Stages::kTileBytes;
@@ -493,10 +493,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
       }
     }
     leave_term(t + kAhead);
-    if (kAhead > 1 && t + kAhead < t_end)
-      wait_vmem_except<3 * Stream::kInsts>();
-    else
-      wait_vmem();
+    wait_vmem();
     __syncthreads();
   };
   again = 0;
@@ -551,12 +548,12 @@ void launch_dq(const DevGeom& g, const AttnOperands& op, const SelectLists& list
   }
 }
 
-template <int D, int kStages, int OCC>
+template <int D, int OCC>
 void launch_dkv(const AttnOperands& op, SelectBwdParams p, hipStream_t stream) {
   p.tiles = blocks_of(op.Nq, kWaves * 16);
   p.by_xcd = true;
   ProfileScope prof("select_attn_bwd_dkv_bf16", stream);
-  select_bwd_dkv_kernel<D, kStages, OCC><<<dim3(work_grid_size(p.tiles, p.BH)), kWaves * 64, 0, stream>>>(p);
+  select_bwd_dkv_kernel<D, OCC><<<dim3(work_grid_size(p.tiles, p.BH)), kWaves * 64, 0, stream>>>(p);
 }
 
 }  // namespace
@@ -597,13 +594,13 @@ hipError_t launch_select_bwd_bf16(const DevGeom& g, const AttnOperands& op, cons
   p.hist_rows = op.hist_rows;
   if (g.D == 128) {
     launch_dq<128, 1, 2, 3>(g, op, lists, p, stream);
-    launch_dkv<128, 2, 2>(op, p, stream);
+    launch_dkv<128, 2>(op, p, stream);
   } else {
     if (lists.query_block % 128 == 0)
       launch_dq<64, 2, 3, 2>(g, op, lists, p, stream);
     else
       launch_dq<64, 1, 3, 3>(g, op, lists, p, stream);
-    launch_dkv<64, 2, 3>(op, p, stream);
+    launch_dkv<64, 3>(op, p, stream);
   }
   return hipGetLastError();
 }
