@@ -234,6 +234,7 @@ class KVCache:
         self._workspace = None
         self._select_bytes = {}  # workspace of the calls over selected blocks, by chunk frames and group
         self._select_spaces = {}  # and one for every stream that such calls were made on
+        self._device_index = None if k_storage is None else k_storage.device.index
         # the desc as plain values: every call checks its tensors against them
         self._dims = (desc.batch, desc.grid_h * desc.grid_w, desc.heads, desc.head_dim)
         self._torch_dtype = torch.bfloat16 if desc.dtype == ASTRO_BF16 else torch.float32
@@ -713,19 +714,26 @@ def _select_bytes(cache: KVCache, n_frames: int, group: int):
     return cache._select_bytes[key]
 
 
+def _is_capturing(device: int) -> bool:
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
+            return torch.cuda.is_current_stream_capturing()
+    return torch.cuda.is_current_stream_capturing()
+
+
 def _select_workspace(cache: KVCache, nbytes: int, stream) -> torch.Tensor:
     """The workspace of a call that was given none: kept for the stream the call goes to, since calls on others may run at the same
     time; of a call that is captured, the graph's own."""
-    device = cache.k_storage.device
     if stream is not None:  # memory belongs to the stream that it is allocated on
         with torch.cuda.stream(stream):
             return _select_workspace(cache, nbytes, None)
-    handle = _cache_stream(cache, None).value or 0
-    if handle and torch.cuda.is_current_stream_capturing():  # (the default stream cannot be)
-        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    space = cache._select_spaces.get(handle)
+    handle = _raw_stream(cache._device_index) if _raw_stream is not None else torch.cuda.current_stream(cache._device_index).cuda_stream
+    captured = handle != 0 and _is_capturing(cache._device_index)  # (the default stream cannot be)
+    space = None if captured else cache._select_spaces.get(handle)
     if space is None or space.numel() < nbytes:
-        space = cache._select_spaces[handle] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        space = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=cache.k_storage.device)
+        if not captured:
+            cache._select_spaces[handle] = space
     return space
 
 
