@@ -284,6 +284,7 @@ def astro_kvcache_create(batch, heads, head_dim, grid_h, grid_w, capacity_frames
         if sb:
             k_sink_storage = torch.zeros(sb, dtype=torch.uint8, device=device)
             desc.k_sink_storage = _ptr(k_sink_storage)
+    _destroy_dropped()
     handle = c_void_p(None)
     k_means = None
     if key_block and not host_only:
@@ -296,9 +297,22 @@ def astro_kvcache_create(batch, heads, head_dim, grid_h, grid_w, capacity_frames
     return cache
 
 
+_dropped = []  # handles of caches that were dropped while a graph was captured
+
+
 def astro_kvcache_destroy(cache: KVCache) -> None:
     handle, cache.handle = cache.handle, None
+    # A free ends a capture with an error, and the garbage collector does not ask: such a handle waits for the next create or destroy.
+    if handle is not None and cache.k_storage is not None and torch.cuda.is_current_stream_capturing():
+        _dropped.append(handle)
+        return
     _check(_lib.astro_kvcache_destroy(handle), "astro_kvcache_destroy")
+    _destroy_dropped()
+
+
+def _destroy_dropped() -> None:
+    while _dropped and not torch.cuda.is_current_stream_capturing():
+        _check(_lib.astro_kvcache_destroy(_dropped.pop()), "astro_kvcache_destroy")
 
 
 def astro_kvcache_reset(cache: KVCache, stream_index: int = -1, start_frame: int = 0) -> None:
