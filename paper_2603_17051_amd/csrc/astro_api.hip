@@ -10,6 +10,7 @@
 #include "../../include/astro.h"
 #include "kernels.hpp"
 #include "ring_state.hpp"
+#include "select_rules.hpp"
 
 using namespace astro;
 
@@ -262,10 +263,11 @@ int check_select_call(const astro_kvcache* c, int n_frames, int group, int query
   return ASTRO_OK;
 }
 
-// bf16: halves of the rotated queries and chunk keys, the temporal table, then parts of a cut forward or the backward's row terms;
+// bf16: halves (and rests) of the rotated queries and chunk keys, the temporal table, then parts of a cut forward or the backward's row terms;
 // fp32: as the dense calls, with <dO, O> of every row in place of the score matrices
 struct SelectSpace : Workspace {
-  size_t q_lo, kc_lo;
+  size_t q_lo, kc_lo, q_rest, kc_rest;
+  bool fine;  // three pieces, not two
 };
 SelectSpace carve_select(const astro_kvcache* c, int n_frames, bool bwd, int group) {
   const RingGeometry& g = c->geo;
@@ -277,17 +279,21 @@ SelectSpace carve_select(const astro_kvcache* c, int n_frames, bool bwd, int gro
     return w;
   }
   const size_t rot = w.kc_rot;
+  w.fine = select_fine(bwd, (int64_t)g.B * group * g.H * nq);
   w.q_lo = 2 * rot;
   w.kc_lo = 3 * rot;
-  w.tab_t += 2 * rot;
-  w.scratch += 2 * rot;
+  w.q_rest = 4 * rot;
+  w.kc_rest = 5 * rot;
+  w.tab_t += (w.fine ? 4 : 2) * rot;
+  w.scratch += (w.fine ? 4 : 2) * rot;
   const DevGeom d = dev_geom(c, group);
   w.total = w.scratch + align256(bwd ? select_bwd_bytes(d, nq) : select_fwd_split_bytes(d, nq));
   return w;
 }
 
 SelectStaged select_staged(char* ws, const SelectSpace& w) {
-  return SelectStaged{ws + w.q_rot, ws + w.q_lo, ws + w.kc_rot, ws + w.kc_lo, (float2*)(ws + w.tab_t)};
+  return SelectStaged{ws + w.q_rot, ws + w.q_lo, ws + w.kc_rot, ws + w.kc_lo, w.fine ? ws + w.q_rest : nullptr, w.fine ? ws + w.kc_rest : nullptr,
+                      (float2*)(ws + w.tab_t)};
 }
 
 // rotated queries and chunk keys into the workspace, which no later call takes for a dense call's

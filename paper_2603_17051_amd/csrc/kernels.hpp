@@ -186,10 +186,10 @@ inline CallShape select_call_shape(const DevGeom& g, const AttnOperands& op, con
   for (int b = 0; b < g.B / op.group; ++b) rows[b] = (int32_t)(op.hist_rows.v[b] < most ? op.hist_rows.v[b] : most);
   return make_call_shape(g.D, g.n_cus, g.B * g.H, op.Nq, op.block_rows, op.in_order, rows, g.B / op.group);
 }
-// Rotated queries (times log2(e)/sqrt(D)) and chunk keys as two bf16 halves each, head-major [B][H][Nq][D], and the temporal pairs'
-// (cos, sin) [B][n_frames][n_t] that turn gradients back.
+// Rotated queries (times log2(e)/sqrt(D)) and chunk keys as two bf16 halves each, head-major [B][H][Nq][D], what those leave of them
+// (null unless select_fine()), and the temporal pairs' (cos, sin) [B][n_frames][n_t] that turn gradients back.
 struct SelectStaged {
-  void *q_hi, *q_lo, *k_hi, *k_lo;
+  void *q_hi, *q_lo, *k_hi, *k_lo, *q_rest, *k_rest;
   float2* tab_t;
 };
 hipError_t launch_select_stage(const DevGeom& g, const void* q, const void* k, const SelectStaged& to, int n_frames,

@@ -34,10 +34,10 @@ struct SelectBwdParams {
 };
 
 // ---- query side: 16 * QS queries of a wave, lane (i = lane % 16, g = lane / 16) owns queries 16 * qs + i ----------------
-template <int D, int QS>
+template <int D, int QS, bool kFine>
 struct SelectDqWave {
   static constexpr int KS = D / 32, DT = D / 16;
-  bf16x8 qh[QS][KS], ql[QS][KS], doreg[QS][KS];
+  bf16x8 qh[QS][KS], ql[QS][KS], qr[kFine ? QS : 1][KS], doreg[QS][KS];
   f32x4 neg_lse2[QS], neg_delta[QS];  // four copies: the accumulators of S and dP start from them
   f32x4 dq[DT][QS];
   OperandAddr16<D> addr;
@@ -56,6 +56,7 @@ struct SelectDqWave {
       for (int st = 0; st < KS; ++st) {
         qh[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_hi + at + st * 32);
         ql[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_lo + at + st * 32);
+        if constexpr (kFine) qr[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_rest + at + st * 32);
         doreg[qs][st] = *reinterpret_cast<const bf16x8*>(p.dout + token + st * 32);
         const bf16x8 o = *reinterpret_cast<const bf16x8*>(p.out + token + st * 32);
 #pragma unroll
@@ -88,14 +89,16 @@ struct SelectDqWave {
   }
 
   template <bool kChunk, bool kCare>  // as in the forward
-  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring = false) {
-    const char *ks = stage, *vs = stage + kSelectTile * D * 2, *lo = stage + 2 * kSelectTile * D * 2;
+  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring) {
+    const char *ks = stage, *vs = stage + kSelectTile * D * 2, *lo = vs + kSelectTile * D * 2;
     f32x4 s[2][QS], dp[2][QS], start[2][QS];
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) start[kh][qs] = neg_lse2[qs];
-    if constexpr (kCare)
+    if constexpr (kFine)
+      scores_from_thirds<D, QS, kCare>(ks, lo, lo + kSelectTile * D * 2, !ring, addr, qh, ql, qr, start, s);
+    else if constexpr (kCare)
       scores_of_any<D, QS>(ks, lo, !ring, addr, qh, ql, start, s);
     else
       scores_from_halves<D, QS, kChunk>(ks, lo, addr, qh, ql, start, s);
@@ -156,7 +159,9 @@ struct SelectDqWave {
             const bf16x8 x = only(mask, read_cols16<D>(ks, addr.tr[dt], 0));
             const f32x4 big = mfma16(x, hi[qs], dq[dt][qs]);
             f32x4 to = mfma16(x, small[qs], big);
-            to = mfma16(only(low_mask, read_cols16<D>(lo, addr.tr[dt], 0)), hi[qs], to);
+            const bf16x8 y = only(low_mask, read_cols16<D>(lo, addr.tr[dt], 0));
+            to = mfma16(y, hi[qs], to);
+            if constexpr (kFine) to = mfma16(y, small[qs], to);
             dq[dt][qs] = either(mine, with_small(big, to), dq[dt][qs]);
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -179,15 +184,16 @@ struct SelectDqWave {
       product(a[quad & 1], hi);
       product(a[quad & 1], small);
       if constexpr (kChunk) product(c[quad & 1], hi);
+      if constexpr (kChunk && kFine) product(c[quad & 1], small);
     }
   }
 };
 
-template <int D, int QS, int kStages, int OCC>
+template <int D, int QS, int kStages, int OCC, bool kFine>
 __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dq_kernel(SelectBwdParams p, SelectLists lists) {
-  using Wave = SelectDqWave<D, QS>;
-  using Walk = SelectWalk<D, kWaves>;
-  using Stages = SelectStages<D, kWaves, kStages>;
+  using Wave = SelectDqWave<D, QS, kFine>;
+  using Walk = SelectWalk<D, kWaves, kFine>;
+  using Stages = SelectStages<D, kWaves, kStages, kFine>;
   constexpr int kAhead = kStages - 1, kQueries = kWaves * 16 * QS;
   __shared__ __attribute__((aligned(1024))) char lds[Stages::kBytes];
   __shared__ TileList tile_list;
@@ -215,6 +221,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dq_kernel(SelectB
   walk.v_ring = segment_words(p.v_cache + (int64_t)pair.cache_bh * p.cache_rows * D, D, 1, D);
   walk.k_hi = segment_words((const __bf16*)p.staged.k_hi + bh * p.Nq * D, D, p.Nq, D);
   walk.k_lo = segment_words((const __bf16*)p.staged.k_lo + bh * p.Nq * D, D, p.Nq, D);
+  if constexpr (kFine) walk.k_rest = segment_words((const __bf16*)p.staged.k_rest + bh * p.Nq * D, D, p.Nq, D);
   walk.v_chunk = segment_words(p.v_chunk + ((int64_t)b * p.Nq * p.H + h) * D, (int64_t)p.H * D, p.Nq, D);
   walk.v_chunk_stride = p.H * D * 2;
   const int t_begin = (int)((int64_t)split * walk.tiles / p.splits), t_end = (int)((int64_t)(split + 1) * walk.tiles / p.splits);
@@ -309,11 +316,11 @@ __global__ void __launch_bounds__(256) select_dq_merge_kernel(SelectBwdParams p,
 }
 
 // ---- key side: 16 chunk keys of a wave, lane (i, g) owns key i; tiles of 32 queries -----------------------------------------
-template <int D, int OCC>
+template <int D, int OCC, bool kFine>
 __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(SelectBwdParams p) {
   constexpr int KS = D / 32, DT = D / 16, kStages = 2, kAhead = kStages - 1, kKeys = kWaves * 16;
   using Stream = SharedStream<D, kWaves>;
-  using Stages = SelectStages<D, kWaves, kStages>;
+  using Stages = SelectStages<D, kWaves, kStages, kFine>;
   constexpr int kTileBytes = Stages::kTileBytes;
   __shared__ __attribute__((aligned(1024))) char lds[Stages::kBytes];
   __shared__ __attribute__((aligned(1024))) float terms[kStages][2][kSelectTile];  // -lse * log2(e), -<dO, O>
@@ -328,7 +335,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
   const int j_wg = item.tile * kKeys, j = j_wg + wave * 16 + i16, j_last = p.Nq - 1;
   OperandAddr16<D> addr;
   addr.init(lane);
-  bf16x8 kh[1][KS], kl[1][KS], v[KS];
+  bf16x8 kh[1][KS], kl[1][KS], kr[1][KS], v[KS];
   {
     const int row = j < p.Nq ? j : j_last;
     const int64_t at = (bh * p.Nq + row) * D + g * 8, token = (((int64_t)b * p.Nq + row) * p.H + h) * D + g * 8;
@@ -336,6 +343,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     for (int st = 0; st < KS; ++st) {
       kh[0][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.k_hi + at + st * 32);
       kl[0][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.k_lo + at + st * 32);
+      if constexpr (kFine) kr[0][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.k_rest + at + st * 32);
       v[st] = *reinterpret_cast<const bf16x8*>(p.v_chunk + token + st * 32);
     }
   }
@@ -350,6 +358,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
   stream.init();
   const u32x4 q_hi = segment_words((const __bf16*)p.staged.q_hi + bh * p.Nq * D, D, p.Nq, D);
   const u32x4 q_lo = segment_words((const __bf16*)p.staged.q_lo + bh * p.Nq * D, D, p.Nq, D);
+  const u32x4 q_rest = kFine ? segment_words((const __bf16*)p.staged.q_rest + bh * p.Nq * D, D, p.Nq, D) : u32x4{};
   const u32x4 dout = segment_words(p.dout + ((int64_t)b * p.Nq * p.H + h) * D, (int64_t)p.H * D, p.Nq, D);
   // a row behind the last query has zeros for Q~ and dO, and a term that makes its P exactly 0 (exp2 of any lse may be infinite)
   const float* const term_rows = (wave & 1 ? p.neg_delta : p.neg_lse2) + bh * p.Nq;
@@ -358,6 +367,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     stream.issue(q_hi, D * 2, t * kSelectTile, stage);
     stream.issue(dout, p.H * D * 2, t * kSelectTile, stage + kTileBytes);
     stream.issue(q_lo, D * 2, t * kSelectTile, stage + 2 * kTileBytes);
+    if constexpr (kFine) stream.issue(q_rest, D * 2, t * kSelectTile, stage + 3 * kTileBytes);
   };
   float term = 0.f;  // of the tile ahead: waves 0 and 1 bring them
   auto take_term = [&](int t) __attribute__((always_inline)) {
@@ -393,7 +403,9 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
     }
     // of the tile's queries: this lane's key is a key of [from, to)
     const int from = min(max(first - t * kSelectTile, 0), kSelectTile), to = min(p.Nq - t * kSelectTile, kSelectTile);
-    if constexpr (kCare)
+    if constexpr (kFine)
+      scores_from_thirds<D, 1, kCare>(qs, lo, lo + kTileBytes, true, addr, kh, kl, kr, start, s);
+    else if constexpr (kCare)
       scores_of_any<D, 1>(qs, lo, true, addr, kh, kl, start, s);
     else
       scores_from_halves<D, 1, true>(qs, lo, addr, kh, kl, start, s);
@@ -456,7 +468,9 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
           const bf16x8 x = only(mask, read_cols16<D>(dos, addr.tr[dt], 0)), y = only(mask, read_cols16<D>(qs, addr.tr[dt], 0));
           const f32x4 big_v = mfma16(x, p_hi, dv[dt]), big_k = mfma16(y, ds_hi, dk[dt]);
           dv[dt] = either(mine, with_small(big_v, mfma16(x, p_lo, big_v)), dv[dt]);
-          const f32x4 all_k = mfma16(only(mask, read_cols16<D>(lo, addr.tr[dt], 0)), ds_hi, mfma16(y, ds_lo, big_k));
+          const bf16x8 z = only(mask, read_cols16<D>(lo, addr.tr[dt], 0));
+          f32x4 all_k = mfma16(z, ds_hi, mfma16(y, ds_lo, big_k));
+          if constexpr (kFine) all_k = mfma16(z, ds_lo, all_k);
           dk[dt] = either(mine, with_small(big_k, all_k), dk[dt]);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -489,6 +503,9 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
         for (int i = 0; i < 4; ++i) dk[4 * quad + i] = mfma16(x[i], ds_lo, dk[4 * quad + i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) dk[4 * quad + i] = mfma16(c[quad & 1][i], ds_hi, dk[4 * quad + i]);
+        if constexpr (kFine)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dk[4 * quad + i] = mfma16(c[quad & 1][i], ds_lo, dk[4 * quad + i]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -527,7 +544,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_bwd_dkv_kernel(Select
   }
 }
 
-template <int D, int QS, int kStages, int OCC>
+template <int D, int QS, int kStages, int OCC, bool kFine>
 void launch_dq(const DevGeom& g, const AttnOperands& op, const SelectLists& lists, SelectBwdParams p, hipStream_t stream) {
   p.tiles = blocks_of(op.Nq, kWaves * 16 * QS);
   const CallShape shape = select_call_shape(g, op, lists);
@@ -538,7 +555,7 @@ void launch_dq(const DevGeom& g, const AttnOperands& op, const SelectLists& list
   p.by_xcd = order_by_xcd(shape, items);
   {
     ProfileScope prof("select_attn_bwd_dq_bf16", stream);
-    select_bwd_dq_kernel<D, QS, kStages, OCC><<<dim3(items), kWaves * 64, 0, stream>>>(p, lists);
+    select_bwd_dq_kernel<D, QS, kStages, OCC, kFine><<<dim3(items), kWaves * 64, 0, stream>>>(p, lists);
   }
   if (p.splits > 1) {
     const uint32_t n_rows = (uint32_t)p.BH * op.Nq;
@@ -548,12 +565,12 @@ void launch_dq(const DevGeom& g, const AttnOperands& op, const SelectLists& list
   }
 }
 
-template <int D, int OCC>
+template <int D, int OCC, bool kFine>
 void launch_dkv(const AttnOperands& op, SelectBwdParams p, hipStream_t stream) {
   p.tiles = blocks_of(op.Nq, kWaves * 16);
   p.by_xcd = true;
   ProfileScope prof("select_attn_bwd_dkv_bf16", stream);
-  select_bwd_dkv_kernel<D, OCC><<<dim3(work_grid_size(p.tiles, p.BH)), kWaves * 64, 0, stream>>>(p);
+  select_bwd_dkv_kernel<D, OCC, kFine><<<dim3(work_grid_size(p.tiles, p.BH)), kWaves * 64, 0, stream>>>(p);
 }
 
 }  // namespace
@@ -592,15 +609,23 @@ hipError_t launch_select_bwd_bf16(const DevGeom& g, const AttnOperands& op, cons
   p.cache_rows = (int64_t)g.C * g.T;
   p.scale = 1.0f / sqrtf((float)g.D);
   p.hist_rows = op.hist_rows;
-  if (g.D == 128) {
-    launch_dq<128, 1, 2, 3>(g, op, lists, p, stream);
-    launch_dkv<128, 2>(op, p, stream);
+  if (staged.q_rest) {  // a few workgroups, each alone on its CU
+    if (g.D == 128) {
+      launch_dq<128, 1, 2, 1, true>(g, op, lists, p, stream);
+      launch_dkv<128, 1, true>(op, p, stream);
+    } else {
+      launch_dq<64, 1, 3, 1, true>(g, op, lists, p, stream);
+      launch_dkv<64, 1, true>(op, p, stream);
+    }
+  } else if (g.D == 128) {
+    launch_dq<128, 1, 2, 3, false>(g, op, lists, p, stream);
+    launch_dkv<128, 2, false>(op, p, stream);
   } else {
     if (lists.query_block % 128 == 0)
-      launch_dq<64, 2, 3, 2>(g, op, lists, p, stream);
+      launch_dq<64, 2, 3, 2, false>(g, op, lists, p, stream);
     else
-      launch_dq<64, 1, 3, 3>(g, op, lists, p, stream);
-    launch_dkv<64, 3>(op, p, stream);
+      launch_dq<64, 1, 3, 3, false>(g, op, lists, p, stream);
+    launch_dkv<64, 3, false>(op, p, stream);
   }
   return hipGetLastError();
 }

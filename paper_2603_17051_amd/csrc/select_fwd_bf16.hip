@@ -35,10 +35,10 @@ struct SelectFwdParams {
 };
 
 // 16 * QS queries of a wave: lane (i = lane % 16, g = lane / 16) owns queries 16 * qs + i.
-template <int D, int QS>
+template <int D, int QS, bool kFine>
 struct SelectFwdWave {
   static constexpr int KS = D / 32, DT = D / 16;
-  bf16x8 qh[QS][KS], ql[QS][KS];
+  bf16x8 qh[QS][KS], ql[QS][KS], qr[kFine ? QS : 1][KS];
   f32x4 o[DT][QS];
   float ref[QS], sum[QS];  // softmax reference in log2 units, this lane's part of the row sum
   OperandAddr16<D> addr;
@@ -109,14 +109,16 @@ struct SelectFwdWave {
   // kCare: with care (see each_bound()), for tiles of both kinds (`ring`: which; a second instance of the careful code moved the registers
   // of the backward's first walk, 1080 -> 1270 us); else what the tile holds has to be finite.
   template <bool kChunk, bool kCare>
-  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring = false) {
-    const char *vs = stage + kSelectTile * D * 2, *lo = stage + 2 * kSelectTile * D * 2;
+  __device__ __forceinline__ void tile(const char* stage, const int (&live)[QS], int fewest, bool ring) {
+    const char *vs = stage + kSelectTile * D * 2, *lo = vs + kSelectTile * D * 2;
     f32x4 s[2][QS], start[2][QS];  // the scores come out relative to the reference
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) start[kh][qs] = f32x4{-ref[qs], -ref[qs], -ref[qs], -ref[qs]};
-    if constexpr (kCare)
+    if constexpr (kFine)
+      scores_from_thirds<D, QS, kCare>(stage, lo, lo + kSelectTile * D * 2, !ring, addr, qh, ql, qr, start, s);
+    else if constexpr (kCare)
       scores_of_any<D, QS>(stage, lo, !ring, addr, qh, ql, start, s);
     else
       scores_from_halves<D, QS, kChunk>(stage, lo, addr, qh, ql, start, s);
@@ -185,11 +187,11 @@ struct SelectFwdWave {
   }
 };
 
-template <int D, int QS, int OCC>
+template <int D, int QS, int OCC, bool kFine>
 __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdParams p, SelectLists lists) {
-  using Wave = SelectFwdWave<D, QS>;
-  using Walk = SelectWalk<D, kWaves>;
-  using Stages = SelectStages<D, kWaves, kStages>;
+  using Wave = SelectFwdWave<D, QS, kFine>;
+  using Walk = SelectWalk<D, kWaves, kFine>;
+  using Stages = SelectStages<D, kWaves, kStages, kFine>;
   constexpr int kAhead = kStages - 1, kQueries = kWaves * 16 * QS;
   __shared__ __attribute__((aligned(1024))) char lds[Stages::kBytes];
   __shared__ TileList tile_list;
@@ -219,6 +221,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
     for (int st = 0; st < Wave::KS; ++st) {
       w.qh[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_hi + at + st * 32);
       w.ql[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_lo + at + st * 32);
+      if constexpr (kFine) w.qr[qs][st] = *reinterpret_cast<const bf16x8*>((const __bf16*)p.staged.q_rest + at + st * 32);
     }
   }
   // The queries have to be here before the first tile is asked for: the compiler does not count the walk's loads, and would wait
@@ -231,6 +234,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
   walk.v_ring = segment_words(p.v_cache + (int64_t)pair.cache_bh * p.cache_rows * D, D, 1, D);
   walk.k_hi = segment_words((const __bf16*)p.staged.k_hi + bh * p.Nq * D, D, p.Nq, D);
   walk.k_lo = segment_words((const __bf16*)p.staged.k_lo + bh * p.Nq * D, D, p.Nq, D);
+  if constexpr (kFine) walk.k_rest = segment_words((const __bf16*)p.staged.k_rest + bh * p.Nq * D, D, p.Nq, D);
   walk.v_chunk = segment_words(p.v_chunk + ((int64_t)b * p.Nq * p.H + h) * D, (int64_t)p.H * D, p.Nq, D);
   walk.v_chunk_stride = p.H * D * 2;
   const int t_begin = (int)((int64_t)split * walk.tiles / p.splits), t_end = (int)((int64_t)(split + 1) * walk.tiles / p.splits);
@@ -338,7 +342,7 @@ __global__ void __launch_bounds__(256) select_merge_kernel(SelectFwdParams p, ui
   if (c == 0) p.lse[lse_at] = m + __logf(tot);
 }
 
-template <int D, int QS, int OCC>
+template <int D, int QS, int OCC, bool kFine>
 hipError_t launch(const DevGeom& g, const AttnOperands& op, const SelectStaged& staged, const SelectLists& lists, void* out, float* lse,
                   float* parts, hipStream_t stream) {
   SelectFwdParams p;
@@ -366,7 +370,7 @@ hipError_t launch(const DevGeom& g, const AttnOperands& op, const SelectStaged& 
   p.lse_part = parts ? parts + p.splits * n_rows * D : nullptr;
   {
     ProfileScope prof("select_attn_fwd_bf16", stream);
-    select_fwd_kernel<D, QS, OCC><<<dim3(work_grid_size(p.q_tiles, p.BH * p.splits)), kWaves * 64, 0, stream>>>(p, lists);
+    select_fwd_kernel<D, QS, OCC, kFine><<<dim3(work_grid_size(p.q_tiles, p.BH * p.splits)), kWaves * 64, 0, stream>>>(p, lists);
   }
   if (p.splits > 1) {
     ProfileScope prof("select_attn_fwd_merge", stream);
@@ -386,9 +390,13 @@ size_t select_fwd_split_bytes(const DevGeom& g, int Nq) {
 hipError_t launch_select_fwd_bf16(const DevGeom& g, const AttnOperands& op, const SelectStaged& staged, const SelectLists& lists, void* out,
                                   float* lse, float* parts, hipStream_t stream) {
   const bool wide = lists.query_block % 128 == 0;
-  if (g.D == 128)
-    return wide ? launch<128, 2, 2>(g, op, staged, lists, out, lse, parts, stream) : launch<128, 1, 2>(g, op, staged, lists, out, lse, parts, stream);
-  return wide ? launch<64, 2, 3>(g, op, staged, lists, out, lse, parts, stream) : launch<64, 1, 3>(g, op, staged, lists, out, lse, parts, stream);
+  auto run = [&](auto f) { return f(g, op, staged, lists, out, lse, parts, stream); };
+  if (staged.q_rest) {  // a few workgroups, each alone on its CU
+    if (g.D == 128) return wide ? run(launch<128, 2, 1, true>) : run(launch<128, 1, 1, true>);
+    return wide ? run(launch<64, 2, 1, true>) : run(launch<64, 1, 1, true>);
+  }
+  if (g.D == 128) return wide ? run(launch<128, 2, 2, false>) : run(launch<128, 1, 2, false>);
+  return wide ? run(launch<64, 2, 3, false>) : run(launch<64, 1, 3, false>);
 }
 
 }  // namespace astro

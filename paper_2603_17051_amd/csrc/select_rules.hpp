@@ -34,6 +34,13 @@ inline int select_splits(const WalkCost& c, int n_cus, int items, double tiles, 
     if (cost(n) < 0.97 * cost(best)) best = n;
   return best;
 }
+// Calls of few rows (queries times heads) form their scores from three pieces of every operand and six products (24 bits), others from two
+// and three (16 bits).  A score's error is that of a probability, 5e-6: over many rows the gradients' 2-norms are 5e-6 to 7e-6 off, hardly
+// more for any inputs (the worst of 150 was 7.3e-6 at 400 rows, 7.0e-6 at 800 and more), but over a few, where one probability may make most of
+// a gradient, up to 1.2e-5 (one in 40 to 140 over 1e-5 at 2 to 48 rows); with three pieces 7e-6.  A log-sum-exp is as near unless it is near 0, which it is in
+// all rows only where there are very few of them.  Few rows wait for latencies: at 128 rows a forward takes 11.3 us from two pieces and 12.6
+// from three.  At the long sizes three would take a third more.
+constexpr bool select_fine(bool bwd, int64_t rows) { return rows <= (bwd ? 512 : 64); }
 // whether a launch of this many rows and pairs may be cut at all (its workspace then has room for the parts)
 inline bool select_may_split(int n_cus, int pairs, int Nq) { return (int64_t)blocks_of(Nq, 128) * pairs < 4 * n_cus; }
 

@@ -90,21 +90,22 @@ struct SharedStream {
   }
 };
 
-// The workgroup's LDS ring of tile stages: K rows, V rows, and for chunk tiles what the rounding of the rotated keys left.
-template <int D, int WAVES, int STAGES>
+// The workgroup's LDS ring of tile stages: K rows, V rows, and for chunk tiles what the rounding of the rotated keys left: a second piece
+// and, if kFine, a third.
+template <int D, int WAVES, int STAGES, bool kFine>
 struct SelectStages {
-  static constexpr int kTileBytes = kSelectTile * D * 2, kBytes = STAGES * 3 * kTileBytes;
-  static __device__ __forceinline__ char* of(char* lds, int t) { return lds + (t % STAGES) * 3 * kTileBytes; }
+  static constexpr int kTileBytes = kSelectTile * D * 2, kTiles = kFine ? 4 : 3, kBytes = STAGES * kTiles * kTileBytes;
+  static __device__ __forceinline__ char* of(char* lds, int t) { return lds + (t % STAGES) * kTiles * kTileBytes; }
 };
 
 // What a workgroup walks: tiles [0, ring_tiles) from the list, then the chunk's rows in order, 32 to a tile, as far as its last
 // query sees them.
-template <int D, int WAVES>
+template <int D, int WAVES, bool kFine>
 struct SelectWalk {
   static constexpr int kTileBytes = kSelectTile * D * 2, kInsts = SharedStream<D, WAVES>::kInsts;
   SharedStream<D, WAVES> stream;
   const TileList* list;
-  u32x4 k_ring, v_ring, k_hi, k_lo, v_chunk;
+  u32x4 k_ring, v_ring, k_hi, k_lo, k_rest, v_chunk;
   uint32_t v_chunk_stride;
   int full, ring_tiles, tiles;
 
@@ -136,6 +137,7 @@ struct SelectWalk {
       stream.issue(k_hi, D * 2, row0, stage);
       stream.issue(v_chunk, v_chunk_stride, row0, stage + kTileBytes);
       stream.issue(k_lo, D * 2, row0, stage + 2 * kTileBytes);
+      if constexpr (kFine) stream.issue(k_rest, D * 2, row0, stage + 3 * kTileBytes);
     }
   }
   // whether any wave of the workgroup has to walk again
@@ -151,7 +153,7 @@ struct SelectWalk {
     else if (newest < ring_tiles)
       wait_vmem_except<2 * kInsts>();
     else
-      wait_vmem_except<3 * kInsts>();
+      wait_vmem_except<(kFine ? 4 : 3) * kInsts>();
   }
 };
 
@@ -257,6 +259,61 @@ __device__ __forceinline__ void scores_of_any(const char* tile, const char* low,
         __builtin_amdgcn_sched_barrier(0);
       }
       s[kh][n] = with_small(big, N == 1 ? big + small : all);
+    }
+}
+
+// Scores from three pieces each: A B^T but for the three smallest products, 24 bits.  rest: A's third pieces; with_low: whether A has more pieces
+// than one.  kCare: as in scores_of_any().
+template <int D, int N, bool kCare>
+__device__ __forceinline__ void scores_from_thirds(const char* tile, const char* low, const char* rest, bool with_low, const OperandAddr16<D>& addr,
+                                                   const bf16x8 (&hi)[N][D / 32], const bf16x8 (&lo)[N][D / 32], const bf16x8 (&third)[N][D / 32],
+                                                   const f32x4 (&start)[2][N], f32x4 (&s)[2][N]) {
+  constexpr int KS = D / 32;
+  f32x4 of_b[2][N], of_a[2][N];  // small products, by whose pieces are small: sums of their own, so that fewer wait for one another
+  bf16x8 a[KS][2], c[KS][2], e[KS][2];
+#pragma unroll
+  for (int st = 0; st < KS; ++st)
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh) {
+      a[st][kh] = read_rows16<D>(tile, addr.row[st], 16 * kh);
+      if (with_low) {
+        c[st][kh] = read_rows16<D>(low, addr.row[st], 16 * kh);
+        e[st][kh] = read_rows16<D>(rest, addr.row[st], 16 * kh);
+      } else {
+        c[st][kh] = e[st][kh] = bf16x8{};
+      }
+    }
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      s[kh][n] = start[kh][n];
+      of_a[kh][n] = of_b[kh][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int st = 0; st < KS; ++st) {
+    auto product = [&](const bf16x8 (&x)[2], const bf16x8 (&y)[N][KS], f32x4 (&to)[2][N]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+        for (int n = 0; n < N; ++n) to[kh][n] = mfma16(x[kh], y[n][st], to[kh][n]);
+    };
+    product(a[st], hi, s);
+    product(a[st], lo, of_b);
+    if (with_low) product(c[st], hi, of_a);
+    product(a[st], third, of_b);
+    if (with_low) {
+      product(c[st], lo, of_a);
+      product(e[st], hi, of_a);
+    }
+  }
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const f32x4 all = s[kh][n] + (of_a[kh][n] + of_b[kh][n]);
+      s[kh][n] = kCare ? with_small(s[kh][n], all) : all;
     }
 }
 
