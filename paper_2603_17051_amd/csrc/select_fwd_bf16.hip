@@ -6,8 +6,8 @@
 //   O^T[d][q]  += V^T P^T            (B = P^T straight from the accumulators of S^T)
 // The scores keep 16 bits of the rotated queries and keys, because the log-sum-exp goes out in fp32 and the backward takes
 // probabilities from it; with operands rounded once it was up to 1e-4 off at 64 keys, now 1e-7 (and the pass 360 us where it is 512
-// now, 4680 queries of 12 heads of 128 over 7168 cached and 4680 chunk keys).  Only P is rounded (the output is bf16): sums are
-// taken of what it was before.  Bound by the products, 3 per cached and 4 per chunk key and query: 578 GFLOP there at 1090 TFLOP/s.
+// now, 4680 queries of 12 heads of 128 over 7168 cached and 4680 chunk keys).  Only P is rounded (the output is bf16): the
+// log-sum-exp is of what it was before, the output's weights are the rounded ones over their sum, so that they sum to 1.  Bound by the products, 3 per cached and 4 per chunk key and query: 578 GFLOP there at 1090 TFLOP/s.
 // A workgroup owns queries of ONE group, turns the group's list into a list of tiles in LDS, and fetches tile after tile
 // through it, two ahead.
 #include "select_rules.hpp"
@@ -40,7 +40,7 @@ struct SelectFwdWave {
   static constexpr int KS = D / 32, DT = D / 16;
   bf16x8 qh[QS][KS], ql[QS][KS], qr[kFine ? QS : 1][KS];
   f32x4 o[DT][QS];
-  float ref[QS], sum[QS];  // softmax reference in log2 units, this lane's part of the row sum
+  float ref[QS], sum[QS], weight[QS];  // softmax reference in log2 units, this lane's parts of the row's sum before and after P is rounded
   OperandAddr16<D> addr;
   int g;
 
@@ -53,7 +53,7 @@ struct SelectFwdWave {
 #pragma unroll
     for (int qs = 0; qs < QS; ++qs) {
       ref[qs] = 0.f;
-      sum[qs] = 0.f;
+      sum[qs] = weight[qs] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt][qs] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -98,6 +98,7 @@ struct SelectFwdWave {
       if (!needed[qs]) less[qs] = 0.f;  // a row's result does not depend on its neighbours
       const float alpha = total[qs] > 0.f ? fast_exp2(-less[qs]) : 0.f;
       sum[qs] *= alpha;
+      weight[qs] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt][qs] = o[dt][qs] * alpha;
       ref[qs] += less[qs];
@@ -136,12 +137,12 @@ struct SelectFwdWave {
     // Probabilities relative to the current reference, which starts at 0 and moves only when a row needs it: its probabilities
     // outgrow it (a huge or infinite sum), or all it has seen are so small that they may vanish.  fp32 sums and bf16's
     // exponents hold what lies between.
-    float part[QS];
+    float part[QS], rounded[QS];
     bf16x8 pb[QS];
     auto probabilities = [&](const float (&less)[QS]) __attribute__((always_inline)) {
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs) {
-        part[qs] = 0.f;
+        part[qs] = rounded[qs] = 0.f;
 #pragma unroll
         for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -149,6 +150,7 @@ struct SelectFwdWave {
             const f32x2 e = {fast_exp2(s[kh][qs][r] - less[qs]), fast_exp2(s[kh][qs][r + 1] - less[qs])};
             part[qs] += e[0] + e[1];
             const bf16x2 x = __builtin_convertvector(e, bf16x2);
+            rounded[qs] = add_pair(x, rounded[qs]);
             pb[qs][4 * kh + r] = x[0];
             pb[qs][4 * kh + r + 1] = x[1];
           }
@@ -161,7 +163,10 @@ struct SelectFwdWave {
     for (int qs = 0; qs < QS; ++qs) look = look || !(part[qs] <= kSumLimit) || !(sum[qs] + part[qs] >= kTiny);
     if (__builtin_expect(__any(look), 0)) move_reference(s, part, probabilities);
 #pragma unroll
-    for (int qs = 0; qs < QS; ++qs) sum[qs] += part[qs];
+    for (int qs = 0; qs < QS; ++qs) {
+      sum[qs] += part[qs];
+      weight[qs] += rounded[qs];
+    }
     if constexpr (kCare) {
 #pragma unroll
       for (int qs = 0; qs < QS; ++qs)
@@ -286,7 +291,7 @@ __global__ void __launch_bounds__(kWaves * 64, OCC) select_fwd_kernel(SelectFwdP
     // a key range in which a query sees nothing reports zeros and a log-sum-exp of -inf, weight 0 in the merge; a sum that is not a number
     // stays one
     const bool nothing = p.splits > 1 && l_tot == 0.f;
-    const float inv = nothing ? 0.f : 1.f / l_tot, lse = w.ref[qs] * kLn2 + __logf(l_tot);
+    const float inv = nothing ? 0.f : 1.f / sum_quarters(w.weight[qs]), lse = w.ref[qs] * kLn2 + __logf(l_tot);
     const int q = q_wave + 16 * qs + i16;
     if (q >= p.Nq) continue;
     const int64_t row = (((int64_t)b * p.Nq + q) * p.H + h) * D + 4 * g;
