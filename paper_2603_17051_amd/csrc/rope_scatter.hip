@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const
   const int64_t in_tok0 = ((int64_t)b * n_frames + fi) * g.T + (int64_t)row * g.gw;
   const int64_t out_row0 = ((int64_t)b * g.H + h) * rows_per_head + dst_frame_row + (int64_t)row * g.gw;
   if constexpr (sizeof(Elem) == 2) {
+    static_assert(kRotateB, "a bf16 append is append_rope_kernel's");
     // kUnroll chunks of each tensor per lane and trip: all their loads are issued before the
     // first is used (2 * kUnroll 16-byte loads in flight per lane), and every element is
     // touched once, so the loads bypass the caches' keep-for-reuse policy.
@@ -145,11 +146,9 @@ __global__ void __launch_bounds__(kThreads) rope_scatter_kernel(DevGeom g, const
             const float a0 = (float)xa[u][2 * v], a1 = (float)xa[u][2 * v + 1];
             xa[u][2 * v] = (__bf16)((a0 * cs.x - a1 * cs.y) * a_scale);
             xa[u][2 * v + 1] = (__bf16)((a0 * cs.y + a1 * cs.x) * a_scale);
-            if constexpr (kRotateB) {
-              const float b0 = (float)xb[u][2 * v], b1 = (float)xb[u][2 * v + 1];
-              xb[u][2 * v] = (__bf16)(b0 * cs.x - b1 * cs.y);
-              xb[u][2 * v + 1] = (__bf16)(b0 * cs.y + b1 * cs.x);
-            }
+            const float b0 = (float)xb[u][2 * v], b1 = (float)xb[u][2 * v + 1];
+            xb[u][2 * v] = (__bf16)(b0 * cs.x - b1 * cs.y);
+            xb[u][2 * v + 1] = (__bf16)(b0 * cs.y + b1 * cs.x);
           }
         }
         if (!rope && a_scale != 1.f) {
