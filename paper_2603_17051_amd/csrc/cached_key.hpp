@@ -23,11 +23,18 @@ __device__ __forceinline__ void exact_temporal(const DevGeom& g, double2* tab_t,
 // The (cos, sin) of four consecutive pairs, the first of them number `pair`, for a token in row `row` and column `col`.
 struct ExactAngles {
   double2 v[4];
-  __device__ __forceinline__ void load(const DevGeom& g, const double2* tab_t, int row, int col, int pair) {
-    const int nb = g.n_t + g.n_h;
+  __device__ __forceinline__ void load_temporal(const DevGeom& g, const double2* tab_t, int pair) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      v[i] = pair + i < g.n_t ? tab_t[pair + i] : pair + i < nb ? g.tab_h64[row * g.n_h + (pair + i - g.n_t)] : g.tab_w64[col * g.n_w + (pair + i - nb)];
+      if (pair + i < g.n_t) v[i] = tab_t[pair + i];
+  }
+  // the others: a token's (one load from a selected address)
+  __device__ __forceinline__ void load_spatial(const DevGeom& g, int row, int col, int pair) {
+    const int nb = g.n_t + g.n_h;
+    const double2 *h = g.tab_h64 + (row * g.n_h - g.n_t), *w = g.tab_w64 + (col * g.n_w - nb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (pair + i >= g.n_t) v[i] = (pair + i < nb ? h : w)[pair + i];
   }
 };
 

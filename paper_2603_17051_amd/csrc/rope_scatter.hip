@@ -65,12 +65,13 @@ __global__ void __launch_bounds__(kThreads) append_rope_kernel(DevGeom g, const 
       }
     }
     ExactAngles at;
-    auto angles = [&](int w) __attribute__((always_inline)) { at.load(g, tab, row, w < g.gw ? w : g.gw - 1, c * 4); };
+    auto angles = [&](int w) __attribute__((always_inline)) { at.load_spatial(g, row, w < g.gw ? w : g.gw - 1, c * 4); };
     if (rope) {
       if (base == 0) {  // under the loads
         exact_temporal(g, tab, first_frame.v[b] + fi);
         __syncthreads();
       }
+      at.load_temporal(g, tab, c * 4);
       angles(base + w0);
     }
 #pragma unroll
@@ -255,7 +256,8 @@ __global__ void __launch_bounds__(kThreads) rope_sink_rerotate_kernel(DevGeom g,
     Chunk x = *reinterpret_cast<const Chunk*>(sink_raw + ((in_tok0 + w) * g.H + h) * g.D + c * EPC);
     if constexpr (kCached) {
       ExactAngles at;
-      at.load(g, tab, row, w, c * 4);
+      at.load_temporal(g, tab, c * 4);
+      at.load_spatial(g, row, w, c * 4);
       x = cached_key8(x, at);
     } else {
 #pragma unroll

@@ -73,9 +73,12 @@ __global__ void __launch_bounds__(kThreads) append_means_kernel(DevGeom g, const
     ExactAngles at;
     auto angles = [&](int r) __attribute__((always_inline)) {
       const int tok = first + (r < n ? r : n - 1), row = tok / g.gw;
-      at.load(g, tab_t, row, tok - row * g.gw, c * 4);
+      at.load_spatial(g, row, tok - row * g.gw, c * 4);
     };
-    if (rope) angles(base + r0);
+    if (rope) {
+      at.load_temporal(g, tab_t, c * 4);
+      angles(base + r0);
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int r = base + u * kRows + r0;
