@@ -2,10 +2,11 @@
 //   P_ij = exp(<Q~_i, K~_j> / sqrt(D) - lse_i),  dS_ij = P_ij (<dO_i, V_j> - <dO_i, O_i>),  j in S_i (see the forward)
 //   dQ~_i = sum over j in S_i of dS_ij K~_j / sqrt(D)       dK~_j = sum over i that see j of dS_ij Q~_i / sqrt(D)
 //   dV_j  = sum over i that see j of P_ij dO_i              (j a chunk row; dQ~ and dK~ are turned back)
-// Gradients go out in fp32 and are as exact: every operand that is not bf16 by itself (rotated queries and chunk keys, P, dS)
+// Gradients go out in fp32 and carry 16 bits: every operand that is not bf16 by itself (rotated queries and chunk keys, P, dS)
 // enters its products as two bf16 halves, the halves' small products left out (2^-17).  With one rounded half each the
-// gradients were 3.8e-3 off, now 6.7e-6; the price is 5 products instead of 3 per cached key, and 7 + 9 instead of 3 + 4 per
-// chunk key: two clips of 4680 rows, 24 pairs of 128, 2816 cached keys 2100 us instead of 1139.  Bound by the products, 1.2 PFLOP/s.
+// gradients were 3.8e-3 off, now 6.7e-6 at the keys as they are cached; the price is 5 products instead of 3 per cached key, and 7 + 9
+// instead of 3 + 4 per chunk key: two clips of 4680 rows, 24 pairs of 128, 2816 cached keys 2080 to 2160 us instead of 1139.  Bound by the
+// products, 1.2 PFLOP/s.  Calls of few rows take three pieces in the scores (select_rules.hpp) and all four products of halves of dS with Q~ and K~.
 // Two launches, no atomics: the query side walks a group's tiles as the forward does and leaves the rows' terms (lse, <dO, O>),
 // the key side walks the queries for 64 chunk keys; every chunk row is a key of all queries that see it, whatever those selected.
 #include "select_rules.hpp"

@@ -4,10 +4,11 @@
 // One pass over the keys with a running reference and sum, everything transposed so that a lane owns queries:
 //   S^T[key][q] = K (Q_hi + Q_lo)^T  (+ K_lo Q_hi^T for the chunk's keys; cached keys are bf16 by definition)
 //   O^T[d][q]  += V^T P^T            (B = P^T straight from the accumulators of S^T)
-// The scores keep 16 bits of the rotated queries and keys, because the log-sum-exp goes out in fp32 and the backward takes
-// probabilities from it; with operands rounded once it was up to 1e-4 off at 64 keys, now 1e-7 (and the pass 360 us where it is 512
-// now, 4680 queries of 12 heads of 128 over 7168 cached and 4680 chunk keys).  Only P is rounded (the output is bf16): the
-// log-sum-exp is of what it was before, the output's weights are the rounded ones over their sum, so that they sum to 1.  Bound by the products, 3 per cached and 4 per chunk key and query: 578 GFLOP there at 1090 TFLOP/s.
+// The scores keep 16 bits of the rotated queries and keys (24 for few rows, see select_rules.hpp), because the log-sum-exp goes out in fp32 and
+// the backward takes probabilities from it; with operands rounded once it was up to 1e-4 off at 64 keys, now 1e-7 (and the pass 360 us where
+// it is 516 now, 4680 queries of 12 heads of 128 over 7168 cached and 4680 chunk keys).  Only P is rounded (the output is bf16): the
+// log-sum-exp is of what it was before, the output's weights are the rounded ones over their sum, so that they sum to 1.  Bound by the
+// products, 3 per cached and 4 per chunk key and query: 578 GFLOP there in 490 us behind the staging, 1180 TFLOP/s.
 // A workgroup owns queries of ONE group, turns the group's list into a list of tiles in LDS, and fetches tile after tile
 // through it, two ahead.
 #include "select_rules.hpp"
